@@ -220,6 +220,7 @@ grp_status grp_release_memory(void);
 
 #define GRP_DTYPE_FP32 0
 #define GRP_DTYPE_BF16 1         /* storage of the input features only; accumulate in fp32 */
+#define GRP_DTYPE_E4M3 2         /* 8 bits (1 + 4 + 3, largest 448); the operators of residual blocks only */
 
 /* Model description (the paper's "GNN Models": GraphSAGE aggregates the neighbours'
  * states by averaging, combines with the node's own state and multiplies by a matrix;
@@ -550,6 +551,79 @@ size_t     grp_gemm_tn_workspace_bytes(int64_t M, int32_t K, int32_t N);
 grp_status grp_gemm_tn(int64_t M, int32_t K, int32_t N, const void* A, int64_t lda,
                        int32_t a_dtype, const float* B, int64_t ldb, float* C, int64_t ldc,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ residual blocks on node embeddings
+ *
+ * The operators of a pre-norm residual block  out = h + W2 act(W1 norm(h))  over the rows of a partition's node embeddings, forward and
+ * backward, in bf16 (and 8 bits for the forward products), and the clipping of its gradient.  Rows may start at any element: 16-byte
+ * aligned rows are faster.  Every call is asynchronous on its stream, allocates nothing and may be captured in a HIP graph (but
+ * grp_gradients_create / _destroy).  All arithmetic is fp32 at least; each output is rounded once.  No atomics: equal inputs, equal bits.
+ * Infinities and NaN come out as the formulas have them. */
+
+/* h = x + r;  y = h / sqrt(mean(h^2) + eps) * weight, row by row (y from h before it is rounded).
+ *   x, r, h  DEV [rows x width] of x_dtype (fp32 or bf16); r NULL: h = x; h NULL: not written; h may be x or r (equal pitches)
+ *   weight   DEV float[width] or NULL (ones)
+ *   y        DEV [rows x width] of y_dtype: fp32, bf16, or e4m3 with scale DEV float[rows] (ignored otherwise):
+ *            scale = max(max|y| / 448, 2^-126), y = e4m3(y / scale): what grp_linear reads as A and a_scale
+ * y must not overlap an input.  width <= 32768.  Errors: GRP_EINVAL, GRP_EUNSUPPORTED, GRP_EHIP.              */
+grp_status grp_rmsnorm(int64_t rows, int32_t width, const void* x, int64_t ldx, int32_t x_dtype, const void* r, int64_t ldr,
+                       const float* weight, float eps, void* h, int64_t ldh, void* y, int64_t ldy, int32_t y_dtype,
+                       float* scale, void* stream);
+/* Rows in 8 bits without a norm: scale = max(max|x| / 448, 2^-126), q = e4m3(x / scale) (activations, or weights once). */
+grp_status grp_quantize_rows(int64_t rows, int32_t width, const void* x, int64_t ldx, int32_t x_dtype, void* q, int64_t ldq,
+                             float* scale, void* stream);
+/* The norm's gradient from its kept h:  u = dy weight, rho = 1 / sqrt(mean(h^2) + eps),
+ *   dh = rho u - h rho^3 mean(u h) + g,   dweight = sum over rows of dy h rho
+ *   dy       DEV of dy_dtype      h, g, dh  DEV of h_dtype; g NULL: nothing added (g: the gradient that reaches h past the norm);
+ *            dh may be h or g (equal pitches), but not dy
+ *   dweight  DEV float[width], overwritten (a fixed order of additions); NULL: not made (then no workspace is needed)
+ *   workspace DEV of grp_rmsnorm_backward_workspace_bytes(rows, width), contents undefined.       Errors: as above, GRP_EWORKSPACE.  */
+size_t     grp_rmsnorm_backward_workspace_bytes(int64_t rows, int32_t width);
+grp_status grp_rmsnorm_backward(int64_t rows, int32_t width, const void* dy, int64_t lddy, int32_t dy_dtype, const void* h,
+                                int64_t ldh, int32_t h_dtype, const float* weight, float eps, const void* g, int64_t ldg,
+                                void* dh, int64_t lddh, float* dweight, void* workspace, size_t workspace_bytes, void* stream);
+
+#define GRP_ACT_NONE 0
+#define GRP_ACT_RELU 1
+#define GRP_ACT_GELU 2           /* z Phi(z), Phi the normal distribution's (erf)           */
+#define GRP_ACT_SILU 3           /* z / (1 + exp(-z))                                        */
+#define GRP_LINEAR_FORWARD 0
+#define GRP_LINEAR_DX      1
+#define GRP_LINEAR_DW      2
+/* Workspace of the three products (DEV, 16-byte aligned, contents undefined); 0: none is needed.  dtype: of A and W. */
+size_t     grp_linear_workspace_bytes(int32_t kind, int64_t M, int32_t N, int32_t K, int32_t dtype);
+/* z = A W + bias;  C = act(z) + r.
+ *   dtype GRP_DTYPE_BF16:  A DEV [M x K], W DEV [K x N] (the layout of a model's parameters); no scales
+ *   dtype GRP_DTYPE_E4M3:  A DEV [M x K], W DEV [N x K], row m of A times a_scale[m] and row n of W times w_scale[n]
+ *                          (DEV float[M], float[N]; NULL: ones), as grp_quantize_rows makes them
+ *   bias  DEV float[N] or NULL      r  DEV [M x N] of c_dtype or NULL; C may be r (equal pitches)
+ *   z     DEV bf16 [M x N] or NULL: the pre-activation, for the backward pass
+ * C DEV [M x N] of c_dtype (fp32 or bf16).  Errors: GRP_EINVAL, GRP_EWORKSPACE, GRP_EUNSUPPORTED, GRP_EHIP.   */
+grp_status grp_linear(int64_t M, int32_t N, int32_t K, const void* A, int64_t lda, const void* W, int64_t ldw, int32_t dtype,
+                      const float* a_scale, const float* w_scale, const float* bias, int32_t act, const void* r, int64_t ldr,
+                      void* C, int64_t ldc, int32_t c_dtype, void* z, int64_t ldz, void* workspace, size_t workspace_bytes,
+                      void* stream);
+/* dA = (dZ W^T) * act'(zin): the gradient that reaches the pre-activation zin (DEV bf16 [M x K]) of the layer below, whose output
+ * act(zin) this layer read; act GRP_ACT_NONE: zin is ignored.  dZ DEV bf16 [M x N], W DEV bf16 [K x N], dA DEV [M x K] of da_dtype. */
+grp_status grp_linear_dx(int64_t M, int32_t N, int32_t K, const void* dZ, int64_t lddz, const void* W, int64_t ldw, int32_t act,
+                         const void* zin, int64_t ldzin, void* dA, int64_t ldda, int32_t da_dtype, void* workspace,
+                         size_t workspace_bytes, void* stream);
+/* dW = A^T dZ and db = column sums of dZ (NULL: not made).  A DEV bf16 [M x K], dZ DEV bf16 [M x N], dW DEV float [K x N]. */
+grp_status grp_linear_dw(int64_t M, int32_t N, int32_t K, const void* A, int64_t lda, const void* dZ, int64_t lddz, float* dW,
+                         int64_t lddw, float* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Clipping by the global norm of a gradient that lies in many tensors.  The handle holds their addresses and a few kilobytes of device
+ * memory, made once for a model's gradient buffers (synchronous); calls that use one handle must not overlap in time.
+ *   src, dst HOST arrays of DEV pointers (dst NULL: in place; an entry equal to src's: that one in place), counts HOST elements,
+ *   dtypes HOST GRP_DTYPE_FP32 / _BF16.  The arrays themselves are copied; the tensors are the caller's and have to outlive the handle.
+ *   Tensors must not overlap each other.                                                                          */
+typedef struct grp_gradients_s grp_gradients_t;
+grp_status grp_gradients_create(int32_t tensors, const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes,
+                                grp_gradients_t** out);
+/* norm = sqrt(sum of the squares of all elements), added in fp64;  dst = src * c, c = 1 if norm <= max_norm else max_norm / norm
+ * (rounded to fp32).  norm_out DEV float[1] or NULL.  Two launches.  Errors: GRP_EINVAL, GRP_EHIP.            */
+grp_status grp_clip_gradients(const grp_gradients_t* gradients, double max_norm, float* norm_out, void* stream);
+grp_status grp_gradients_destroy(grp_gradients_t* gradients);   /* NULL is a no-op */
 
 /* ------------------------------------------------------------------ tuning */
 

@@ -12,7 +12,9 @@ LIB_PATH = os.path.join(_HERE, "libgrappa_hip.so")
 
 GRP_MAX_LAYERS = 16
 ARCH_SAGE_MEAN, ARCH_GCN, ARCH_GCN_RESIDUAL, ARCH_GAT = 0, 1, 2, 3
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+LINEAR_FORWARD, LINEAR_DX, LINEAR_DW = 0, 1, 2
 EST_NONE, EST_NODE_LEVEL, EST_BATCH_MIN_DIST, EST_SHRINKAGE = 0, 1, 2, 3
 OPT_SGD, OPT_ADAM = 0, 1
 SCALE_NONE, SCALE_MEAN, SCALE_RSQRT = 0, 1, 2
@@ -107,6 +109,15 @@ def load() -> C.CDLL:
         "grp_gemm_nn": [i64, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp],
         "grp_gemm_nt": [i64, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp],
         "grp_gemm_tn": [i64, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, sz, vp],
+        "grp_rmsnorm": [i64, i32, vp, i64, i32, vp, i64, vp, C.c_float, vp, i64, vp, i64, i32, vp, vp],
+        "grp_quantize_rows": [i64, i32, vp, i64, i32, vp, i64, vp, vp],
+        "grp_rmsnorm_backward": [i64, i32, vp, i64, i32, vp, i64, i32, vp, C.c_float, vp, i64, vp, i64, vp, vp, sz, vp],
+        "grp_linear": [i64, i32, i32, vp, i64, vp, i64, i32, vp, vp, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, sz, vp],
+        "grp_linear_dx": [i64, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, sz, vp],
+        "grp_linear_dw": [i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp],
+        "grp_gradients_create": [i32, vp, vp, vp, vp, C.POINTER(vp)],
+        "grp_clip_gradients": [vp, C.c_double, vp, vp],
+        "grp_gradients_destroy": [vp],
         "grp_set_slice_policy": [i64, C.c_int32],
         "grp_controller_create": [i64, i32, C.c_double, i64, C.POINTER(vp)],
         "grp_controller_observe": [vp, vp, i32],
@@ -129,6 +140,10 @@ def load() -> C.CDLL:
     lib.grp_super_epoch_epochs.restype = i64
     lib.grp_gemm_tn_workspace_bytes.argtypes = [i64, i32, i32]
     lib.grp_gemm_tn_workspace_bytes.restype = sz
+    lib.grp_rmsnorm_backward_workspace_bytes.argtypes = [i64, i32]
+    lib.grp_rmsnorm_backward_workspace_bytes.restype = sz
+    lib.grp_linear_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+    lib.grp_linear_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -534,6 +549,88 @@ def grp_gemm_tn(M, K, N, A, lda, a_dtype, B, ldb, Cm, ldc, workspace, stream=Non
                               _stream(stream)))
 
 
+def _size(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def grp_rmsnorm(rows, width, x, ldx, x_dtype, r, ldr, weight, eps, h, ldh, y, ldy, y_dtype, scale=None, stream=None):
+    """``y = rmsnorm(x + r) * weight`` and ``h = x + r`` (``r``, ``h``, ``weight``: None where there is none)."""
+    _check(load().grp_rmsnorm(rows, width, _ptr(x), ldx, x_dtype, _ptr(r), ldr, _ptr(weight), eps, _ptr(h), ldh, _ptr(y), ldy, y_dtype, _ptr(scale),
+                              _stream(stream)))
+
+
+def grp_quantize_rows(rows, width, x, ldx, x_dtype, q, ldq, scale, stream=None):
+    """Rows of ``x`` as e4m3 numbers ``q`` times ``scale`` (float32 [rows])."""
+    _check(load().grp_quantize_rows(rows, width, _ptr(x), ldx, x_dtype, _ptr(q), ldq, _ptr(scale), _stream(stream)))
+
+
+def grp_rmsnorm_backward_workspace_bytes(rows, width) -> int:
+    return int(load().grp_rmsnorm_backward_workspace_bytes(rows, width))
+
+
+def grp_rmsnorm_backward(rows, width, dy, lddy, dy_dtype, h, ldh, h_dtype, weight, eps, g, ldg, dh, lddh, dweight, workspace, stream=None):
+    _check(load().grp_rmsnorm_backward(rows, width, _ptr(dy), lddy, dy_dtype, _ptr(h), ldh, h_dtype, _ptr(weight), eps, _ptr(g), ldg, _ptr(dh), lddh,
+                                       _ptr(dweight), _ptr(workspace), _size(workspace), _stream(stream)))
+
+
+def grp_linear_workspace_bytes(kind, M, N, K, dtype) -> int:
+    return int(load().grp_linear_workspace_bytes(kind, M, N, K, dtype))
+
+
+def grp_linear(M, N, K, A, lda, W, ldw, dtype, a_scale, w_scale, bias, act, r, ldr, Cm, ldc, c_dtype, z, ldz, workspace, stream=None):
+    """``Cm = act(A W + bias) + r``; ``W`` is [K x N] in bf16, [N x K] in e4m3 (with the rows' scales)."""
+    _check(load().grp_linear(M, N, K, _ptr(A), lda, _ptr(W), ldw, dtype, _ptr(a_scale), _ptr(w_scale), _ptr(bias), act, _ptr(r), ldr, _ptr(Cm), ldc,
+                             c_dtype, _ptr(z), ldz, _ptr(workspace), _size(workspace), _stream(stream)))
+
+
+def grp_linear_dx(M, N, K, dZ, lddz, W, ldw, act, zin, ldzin, dA, ldda, da_dtype, workspace, stream=None):
+    _check(load().grp_linear_dx(M, N, K, _ptr(dZ), lddz, _ptr(W), ldw, act, _ptr(zin), ldzin, _ptr(dA), ldda, da_dtype, _ptr(workspace),
+                                _size(workspace), _stream(stream)))
+
+
+def grp_linear_dw(M, N, K, A, lda, dZ, lddz, dW, lddw, db, workspace, stream=None):
+    _check(load().grp_linear_dw(M, N, K, _ptr(A), lda, _ptr(dZ), lddz, _ptr(dW), lddw, _ptr(db), _ptr(workspace), _size(workspace), _stream(stream)))
+
+
+class Gradients:
+    """Owns a grp_gradients_t handle (the tensors of a model's gradient) and keeps the tensors alive."""
+
+    def __init__(self, handle: int, tensors):
+        self.handle, self._keep = handle, tensors
+
+    def destroy(self):
+        if self.handle:
+            _check(load().grp_gradients_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def grp_gradients_create(grads, outs=None) -> Gradients:
+    """``grads``: contiguous float32 or bfloat16 device tensors; ``outs``: tensors of the same shapes and types for the clipped gradient (None: in
+    place)."""
+    kinds = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    for i, t in enumerate(grads):
+        o = t if outs is None else outs[i]
+        if t.dtype not in kinds or not t.is_contiguous() or not o.is_contiguous() or o.dtype != t.dtype or o.numel() != t.numel():
+            raise ValueError(f"tensor {i}: contiguous float32 or bfloat16 is needed, and an output of the same type and size")
+    n = len(grads)
+    ptrs = lambda ts: (C.c_void_p * n)(*[_ptr(t) for t in ts])
+    out = C.c_void_p()
+    _check(load().grp_gradients_create(n, ptrs(grads), None if outs is None else ptrs(outs), (C.c_int64 * n)(*[t.numel() for t in grads]),
+                                       (C.c_int32 * n)(*[kinds[t.dtype] for t in grads]), C.byref(out)))
+    return Gradients(out.value, (list(grads), None if outs is None else list(outs)))
+
+
+def grp_clip_gradients(gradients: Gradients, max_norm: float, norm_out=None, stream=None):
+    """Scales the tensors of ``gradients`` by ``max_norm / norm`` where their global norm is above ``max_norm``; the norm goes to ``norm_out``."""
+    _check(load().grp_clip_gradients(gradients.handle, max_norm, _ptr(norm_out), _stream(stream)))
+
+
 def grp_release_memory():
     """Gives back the device memory that the library keeps for later builds on the current GPU."""
     _check(load().grp_release_memory())
@@ -572,4 +669,6 @@ def exported_symbols():
             "grp_partition_destroy", "grp_release_memory", "grp_chunks_build", "grp_chunks_build_assigned", "grp_chunks_destroy", "grp_partition_from_chunks",
             "grp_partition_base_mask", "grp_partition_halo", "grp_param_count", "grp_step_workspace_bytes", "grp_step_activation", "grp_step_block", "grp_train_step", "grp_train_steps",
             "grp_aggregate", "grp_aggregate_ptrs", "grp_optimizer_step", "grp_spmm", "grp_spmm_workspace_bytes", "grp_spmm_static", "grp_gemm_nn", "grp_gemm_nt", "grp_gemm_tn_workspace_bytes", "grp_gemm_tn",
+            "grp_rmsnorm", "grp_quantize_rows", "grp_rmsnorm_backward_workspace_bytes", "grp_rmsnorm_backward", "grp_linear_workspace_bytes", "grp_linear", "grp_linear_dx", "grp_linear_dw",
+            "grp_gradients_create", "grp_clip_gradients", "grp_gradients_destroy",
             "grp_set_slice_policy", "grp_sweep_chunk", "grp_super_epoch_epochs", "grp_controller_create", "grp_controller_observe", "grp_controller_observe_stats", "grp_controller_end_epoch", "grp_controller_state", "grp_controller_destroy", "grp_profile_enable", "grp_profile_report"]

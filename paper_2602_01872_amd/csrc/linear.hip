@@ -1,0 +1,532 @@
+// Linear layers in bf16 and in 8 bits on the matrix cores, with what stands around them in a residual block, and their gradients:
+//
+//   forward   z = A W + b  (8 bits: row m of A times a_scale[m], column n of W times w_scale[n]),  c = act(z) + r       sum over k
+//   dx        dA = (dZ W^T) act'(zin)                                                                                     sum over n
+//   dw        dW = A^T dZ,  db = column sums of dZ                                                                        sum over the rows
+//
+// The 8-bit matrix instructions cut, of every eight products, what is below 2^-13 of the largest (measured on single instructions; rms 1.3e-5 of the
+// result on normal deviates), so e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those.
+//
+// All are one kernel, D[i, j] = sum_s P(i, s) Q(s, j): an operand either has s contiguous ("rows": A, dZ, the 8-bit weights) or its output index
+// ("columns": W of the forward product, both operands of dw).  Products are accumulated in fp32 by the matrix unit.
+//
+// Tiles.  A workgroup of WI x WJ wavefronts makes 16 FI WI rows and 64 WJ columns; a step takes 128 bytes of s (64 bf16, 128 e4m3 numbers) of both operands
+// through LDS, two steps' tiles in turn, so that a step's loads have the whole step before to arrive.
+//   rows     LDS row o (output index) has 128 bytes, eight places of 16; a lane's operand of a matrix instruction is one (bf16) or two (8 bits) places
+//   columns  LDS row s has the tile's output indices; ds_read_b64_tr_b16 turns four rows of 16 around into a lane's four consecutive s
+// Places are permuted by some bits of the row (swizzle) so that the 16 lanes of a group read different banks.
+//   The instruction's rows are D's columns: lane (g, t) holds D[i + t, j + 16 g + 4 f + e], e < 4, for the wavefront's fragments f < 4, that is 16
+// consecutive columns of one row: the epilogue loads and stores 32 or 64 bytes of a row at a time straight from registers.
+#include "common.h"
+
+namespace grp {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+enum LinearOp { FWD_BF16, FWD_E4M3, GRAD_X, GRAD_W };
+constexpr int elem_size(int op) { return op == FWD_E4M3 ? 1 : 2; }
+constexpr bool p_columns(int op) { return op == GRAD_W; }
+constexpr bool q_columns(int op) { return op == GRAD_W || op == FWD_BF16; }
+
+struct LinearArgs {
+    const void* P;
+    int64_t ldp;
+    const void* Q;
+    int64_t ldq;
+    int64_t I, S;                     // rows of D, length of the sums
+    int32_t J;                        // columns of D
+    const float *a_scale, *w_scale, *bias;
+    int32_t act;
+    const void* r;                    // of c's type, or null
+    int64_t ldr;
+    void* c;
+    int64_t ldc;
+    int32_t c_bf16;
+    void* z;                          // forward: out, or null; dx: zin
+    int64_t ldz;
+    float* db;                        // dw
+    float* part;                      // [splits][rows of D (dw: one more, db)][ld_part] when splits > 1
+    int32_t splits, ld_part;
+    int64_t steps_per_split;
+    int32_t tiles_i, tiles_j;
+};
+
+// ------------------------------------------------------------------ epilogue
+__device__ __forceinline__ float act_of(float z, int act) {
+    switch (act) {
+        case GRP_ACT_RELU: return z > 0.f ? z : 0.f;
+        case GRP_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case GRP_ACT_SILU: return z / (1.f + expf(-z));
+        default: return z;
+    }
+}
+__device__ __forceinline__ float slope_of(float z, int act) {
+    switch (act) {
+        case GRP_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case GRP_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+        case GRP_ACT_SILU: { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
+        default: return 1.f;
+    }
+}
+
+// N (a multiple of 4; of 8 for 16-byte accesses of bf16) consecutive elements of which the first n exist.
+template <int N> __device__ __forceinline__ void load_row(const void* p, bool bf16, int n, float (&f)[N]) {
+    if (n >= N) {
+        if (bf16) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                const u32x2_any t = *reinterpret_cast<const u32x2_any*>((const uint16_t*)p + k);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { f[k + 2 * i] = __uint_as_float(t[i] << 16); f[k + 2 * i + 1] = __uint_as_float(t[i] & 0xFFFF0000u); }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) {
+                const u32x4_any t = *reinterpret_cast<const u32x4_any*>((const float*)p + k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[k + i] = __uint_as_float(t[i]);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        f[e] = 0.f;
+        if (e < n) f[e] = bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[e] << 16) : ((const float*)p)[e];
+    }
+}
+template <int N> __device__ __forceinline__ void store_row(void* p, bool bf16, int n, const float (&f)[N]) {
+    if (n >= N) {
+        if (bf16) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4)
+                *reinterpret_cast<u32x2_any*>((uint16_t*)p + k) = u32x2_any{__builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{f[k], f[k + 1]}), bf16x2)),
+                                                                            __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{f[k + 2], f[k + 3]}), bf16x2))};
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k += 4)
+                *reinterpret_cast<u32x4_any*>((float*)p + k) =
+                    u32x4_any{__float_as_uint(f[k]), __float_as_uint(f[k + 1]), __float_as_uint(f[k + 2]), __float_as_uint(f[k + 3])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e < n) {
+            if (bf16) ((__bf16*)p)[e] = (__bf16)f[e];
+            else ((float*)p)[e] = f[e];
+        }
+}
+
+// What depends on the columns alone.
+template <int OP, int N> struct ColumnTerms {
+    float bias[N], ws[N];
+    __device__ __forceinline__ ColumnTerms(const LinearArgs& a, int j) {
+        const int n = a.J - j;
+        if constexpr (OP == FWD_BF16 || OP == FWD_E4M3) {
+            if (a.bias && n > 0) {
+                load_row<N>(a.bias + j, false, n, bias);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) bias[e] = 0.f;
+            }
+        }
+        if constexpr (OP == FWD_E4M3) {
+            if (a.w_scale && n > 0) {
+                load_row<N>(a.w_scale + j, false, n, ws);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) ws[e] = 1.f;
+            }
+        }
+    }
+};
+
+// D[i, j .. j + N - 1], all terms of the sums in v, to the outputs.
+template <int OP, int N> __device__ __forceinline__ void finish(const LinearArgs& a, int64_t i, int j, float (&v)[N], const ColumnTerms<OP, N>& col) {
+    const int n = a.J - j;
+    if (n <= 0) return;
+    if constexpr (OP == FWD_BF16 || OP == FWD_E4M3) {
+        if constexpr (OP == FWD_E4M3) {
+            const float as = a.a_scale ? a.a_scale[i] : 1.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = v[e] * as * col.ws[e];
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] += col.bias[e];
+        if (a.z) store_row<N>((uint16_t*)a.z + i * a.ldz + j, true, n, v);
+        if (a.act != GRP_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = act_of(v[e], a.act);
+        }
+        if (a.r) {
+            float t[N];
+            load_row<N>((const char*)a.r + (i * a.ldr + j) * (a.c_bf16 ? 2 : 4), a.c_bf16, n, t);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] += t[e];
+        }
+    } else if constexpr (OP == GRAD_X) {
+        if (a.act != GRP_ACT_NONE) {
+            float t[N];
+            load_row<N>((const uint16_t*)a.z + i * a.ldz + j, true, n, t);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] *= slope_of(t[e], a.act);
+        }
+    }
+    store_row<N>((char*)a.c + (i * a.ldc + j) * (a.c_bf16 ? 2 : 4), a.c_bf16, n, v);
+}
+
+// ------------------------------------------------------------------ tiles
+// Where place `pos` (16 bytes) of LDS row `row` comes from; an involution.  T: output indices of the tile.
+template <bool COLUMNS, bool IS_Q, int T> __device__ __forceinline__ int swizzle(int pos, int row) {
+    if constexpr (!COLUMNS)
+        return IS_Q ? pos ^ (((row >> 1) & 1) | ((row >> 3) & 6))      // its lanes read rows 16 q + 4 f + e, q and e < 4
+                    : pos ^ ((row >> 1) & 7);                          //                rows t < 16
+    else if constexpr (IS_Q)
+        return T >= 128 ? pos ^ ((row & 1) | ((row & 2) << 2)) : pos ^ ((row >> 1) & 1);
+    else
+        return T >= 128 ? pos ^ (((row & 3) << 1) | (row & 8)) : pos ^ ((row & 2) | ((row >> 1) & 4));
+}
+
+// 16 bytes of which the first n elements of ES bytes exist, the rest as zeros.
+template <int ES> __device__ __forceinline__ u32x4_al load_part(const char* p, int64_t n) {
+    if (n >= 16 / ES) return (u32x4_al)*reinterpret_cast<const u32x4_b*>(p);
+    u32x4_al v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 16 / ES; ++e)
+        if (e < n) {
+            const uint32_t x = ES == 2 ? (uint32_t)((const uint16_t*)p)[e] : (uint32_t)((const uint8_t*)p)[e];
+            v[e * ES / 4] |= x << (8 * (e * ES % 4));
+        }
+    return v;
+}
+
+// Unit u (16 bytes, in the order of LDS) of an operand's tile that starts at output index o0 and s0.
+template <int ES, bool COLUMNS, bool IS_Q, int T>
+__device__ __forceinline__ u32x4_al load_unit(const void* base, int64_t ld, int64_t o0, int64_t O, int64_t s0, int64_t S, int u) {
+    if constexpr (!COLUMNS) {
+        const int row = u >> 3, at = swizzle<COLUMNS, IS_Q, T>(u & 7, row);
+        const int64_t o = o0 + row < O ? o0 + row : O - 1, s = s0 + at * (16 / ES);      // (a row past the end: any; it is not stored)
+        return load_part<ES>((const char*)base + (o * ld + s) * ES, S - s);
+    } else {
+        const int row = u / (T / 8), at = swizzle<COLUMNS, IS_Q, T>(u % (T / 8), row);
+        const int64_t s = s0 + row, o = o0 + at * 8;
+        return load_part<ES>((const char*)base + (s * ld + o) * ES, s < S ? O - o : 0);
+    }
+}
+
+// 16 e4m3 numbers in bf16 (exact).
+struct Wide8 {
+    bf16x8 v[2];
+    Wide8() = default;
+    __device__ __forceinline__ explicit Wide8(u32x4_al x) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bf16x2 t[4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                t[2 * k] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * h + k], 1.f, false);
+                t[2 * k + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * h + k], 1.f, true);
+            }
+            v[h] = bf16x8{t[0][0], t[0][1], t[1][0], t[1][1], t[2][0], t[2][1], t[3][0], t[3][1]};
+        }
+    }
+};
+
+template <int OP, int WI, int WJ, int FI> __global__ __launch_bounds__(64 * WI * WJ) void linear_kernel(LinearArgs a) {
+    constexpr int ES = elem_size(OP), NT = 64 * WI * WJ, TI = 16 * FI * WI, TJ = 64 * WJ, STEP = 128 / ES;
+    constexpr bool PC = p_columns(OP), QC = q_columns(OP);
+    constexpr int UP = TI * 8 / NT, UQ = TJ * 8 / NT;
+    __shared__ __attribute__((aligned(16))) char lds[2][(TI + TJ) * 128];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, t = lane & 15;
+    const int wi = wave / WJ, wj = wave % WJ;
+    const int tile = blockIdx.x % (unsigned)(a.tiles_i * a.tiles_j), split = blockIdx.x / (unsigned)(a.tiles_i * a.tiles_j);
+    const int ti = tile / a.tiles_j, tj = tile % a.tiles_j;
+    const int64_t i0 = (int64_t)ti * TI, j0 = (int64_t)tj * TJ;
+    const int64_t s_begin = split * a.steps_per_split * STEP;
+    const int64_t s_end = s_begin + a.steps_per_split * STEP < a.S ? s_begin + a.steps_per_split * STEP : a.S;
+
+    u32x4_al raw[UP + UQ];
+    auto request = [&](int64_t s0) {
+#pragma unroll
+        for (int n = 0; n < UP; ++n) raw[n] = load_unit<ES, PC, false, TI>(a.P, a.ldp, i0, a.I, s0, a.S, n * NT + threadIdx.x);
+#pragma unroll
+        for (int n = 0; n < UQ; ++n) raw[UP + n] = load_unit<ES, QC, true, TJ>(a.Q, a.ldq, j0, a.J, s0, a.S, n * NT + threadIdx.x);
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int n = 0; n < UP + UQ; ++n)
+            *reinterpret_cast<u32x4_al*>(lds[buf] + ((n < UP ? n * NT : TI * 8 + (n - UP) * NT) + threadIdx.x) * 16) = raw[n];
+    };
+
+    floatx4 acc[FI][4], sums[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[i][f] = floatx4{0.f, 0.f, 0.f, 0.f};
+        sums[f] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const bool make_sums = OP == GRAD_W && ti == 0 && wi == 0 && a.db;
+
+    // byte of a lane's first operand; of the others see at_p, at_q
+    auto at_p = [&](int f, int s, int half) {
+        if constexpr (PC) {
+            const int row = 32 * s + 8 * g + 4 * half + (t >> 2);
+            return row * (TI * 2) + 16 * swizzle<PC, false, TI>((wi * FI + f) * 2 + ((t >> 1) & 1), row) + 8 * (t & 1);
+        } else {
+            const int row = (wi * FI + f) * 16 + t;
+            return row * 128 + 16 * swizzle<PC, false, TI>(4 * s + g, row);
+        }
+    };
+    auto at_q = [&](int f, int s, int half) {
+        if constexpr (QC) {
+            const int row = 32 * s + 8 * g + 4 * half + (t >> 2);
+            return TI * 128 + row * (TJ * 2) + 16 * swizzle<QC, true, TJ>(wj * 8 + (t & 3) * 2 + (f >> 1), row) + 8 * (f & 1);
+        } else {
+            const int row = wj * 64 + (t >> 2) * 16 + f * 4 + (t & 3);
+            return TI * 128 + row * 128 + 16 * swizzle<QC, true, TJ>(4 * s + g, row);
+        }
+    };
+    auto read = [&](const char* buf, auto columns, auto at, int f, int s) -> u32x4_al {
+        if constexpr (decltype(columns)::value) {
+            typedef shortx4 __attribute__((address_space(3))) * tr_ptr;
+            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(buf + at(f, s, 0)));
+            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(buf + at(f, s, 1)));
+            return __builtin_bit_cast(u32x4_al, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *reinterpret_cast<const u32x4_al*>(buf + at(f, s, 0));
+        }
+    };
+
+    if (s_begin < s_end) {
+        request(s_begin);
+        put(0);
+        int buf = 0;
+        for (int64_t s0 = s_begin; s0 < s_end; s0 += STEP, buf ^= 1) {
+            __syncthreads();
+            const bool more = s0 + STEP < s_end;
+            if (more) request(s0 + STEP);
+            const char* const L = lds[buf];
+            if constexpr (ES == 1) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    Wide8 q[4];
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) q[f] = Wide8(*reinterpret_cast<const u32x4_al*>(L + at_q(f, s, 0)));
+#pragma unroll
+                    for (int i = 0; i < FI; ++i) {
+                        const Wide8 p(*reinterpret_cast<const u32x4_al*>(L + at_p(i, s, 0)));
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f].v[h], p.v[h], acc[i][f], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    bf16x8 q[4];
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) q[f] = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, QC>(), at_q, f, s));
+#pragma unroll
+                    for (int i = 0; i < FI; ++i) {
+                        const bf16x8 p = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, PC>(), at_p, i, s));
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], p, acc[i][f], 0, 0, 0);
+                    }
+                    if constexpr (OP == GRAD_W) {
+                        if (make_sums) {
+                            const bf16x8 one = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+                            for (int f = 0; f < 4; ++f) sums[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], one, sums[f], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+            if (more) put(buf ^ 1);
+        }
+    }
+
+    const int j = (int)j0 + wj * 64 + g * 16;
+    if (j >= a.J) return;
+    if (a.splits > 1) {
+        const int64_t rows = a.I + (OP == GRAD_W ? 1 : 0);
+        float* const part = a.part + (int64_t)split * rows * a.ld_part;
+#pragma unroll
+        for (int i = 0; i < FI; ++i) {
+            const int64_t row = i0 + (wi * FI + i) * 16 + t;
+            if (row < a.I)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + row * a.ld_part + j + 4 * f) = acc[i][f];
+        }
+        if (OP == GRAD_W && make_sums && t == 0)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + a.I * a.ld_part + j + 4 * f) = sums[f];
+        return;
+    }
+    const ColumnTerms<OP, 16> col(a, j);
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+        const int64_t row = i0 + (wi * FI + i) * 16 + t;
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = acc[i][e >> 2][e & 3];
+        if (row < a.I) finish<OP, 16>(a, row, j, v, col);
+    }
+    if (OP == GRAD_W && make_sums && t == 0) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = sums[e >> 2][e & 3];
+        store_row<16>(a.db + j, false, a.J - j, v);
+    }
+}
+
+// The partial results of all splits, added in their order, to the outputs: four columns a thread.
+template <int OP> __global__ __launch_bounds__(256) void linear_sum_kernel(LinearArgs a) {
+    const int quads = a.ld_part / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / quads, rows = a.I + (OP == GRAD_W ? 1 : 0);
+    if (row >= rows) return;
+    const int j = (int)(at % quads) * 4;
+    floatx4 s = {0.f, 0.f, 0.f, 0.f};
+    const float* p = a.part + row * a.ld_part + j;
+    in_order(0, a.splits, [&](int k) { return *reinterpret_cast<const floatx4*>(p + (int64_t)k * rows * a.ld_part); },
+             [&](floatx4 v, bool on) { if (on) s += v; });
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    if (OP == GRAD_W && row == a.I) {
+        if (a.db) store_row<4>(a.db + j, false, a.J - j, v);
+        return;
+    }
+    finish<OP, 4>(a, row, j, v, ColumnTerms<OP, 4>(a, j));
+}
+
+// ------------------------------------------------------------------ host
+struct LinearPlan {
+    int64_t steps = 0, per_split = 0;
+    int32_t tiles_i = 0, tiles_j = 0, splits = 1, ld_part = 0;
+    size_t bytes = 0;
+};
+constexpr int64_t MOST_TILES = (int64_t)1 << 30;
+
+LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
+    LinearPlan p;
+    p.tiles_i = (int32_t)cdiv(I, 128);
+    p.tiles_j = (int32_t)cdiv(J, 128);
+    p.steps = cdiv(S, 128 / elem_size(op));
+    const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j;
+    int64_t splits = tiles < 256 ? std::min<int64_t>(cdiv(512, tiles), cdiv(p.steps, 4)) : 1;
+    if (splits < 1) splits = 1;
+    p.per_split = std::max<int64_t>(1, cdiv(p.steps, splits));
+    p.splits = (int32_t)std::max<int64_t>(1, cdiv(p.steps, p.per_split));
+    p.ld_part = (int32_t)round_up(J, 16);
+    if (p.splits > 1) p.bytes = (size_t)p.splits * (size_t)(I + (op == GRAD_W ? 1 : 0)) * p.ld_part * sizeof(float);
+    return p;
+}
+
+template <int OP> grp_status run_linear(const char* who, const char* name, LinearArgs a, double bytes, void* ws, size_t ws_bytes, hipStream_t st) {
+    const LinearPlan p = plan_of(OP, a.I, a.J, a.S);
+    if ((int64_t)p.tiles_i * p.tiles_j * p.splits > MOST_TILES) return fail(GRP_EUNSUPPORTED, "%s: too large", who);
+    if (p.bytes && (!ws || ws_bytes < p.bytes)) return fail(GRP_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : (size_t)0, p.bytes);
+    if (p.bytes && (uintptr_t)ws % 16) return fail(GRP_EINVAL, "%s: workspace is not 16-byte aligned", who);
+    a.part = (float*)ws;
+    a.splits = p.splits;
+    a.ld_part = p.ld_part;
+    a.steps_per_split = p.per_split;
+    a.tiles_i = p.tiles_i;
+    a.tiles_j = p.tiles_j;
+    {
+        ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
+        hipLaunchKernelGGL((linear_kernel<OP, 2, 2, 4>), dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3(256), 0, st, a);
+        GRP_LAUNCH_CHECK();
+    }
+    if (p.splits > 1) {
+        const int64_t rows = a.I + (OP == GRAD_W ? 1 : 0);
+        ProfScope ps("linear_sum", st, 0.0, 4.0 * rows * a.J * (p.splits + 1.0));
+        hipLaunchKernelGGL((linear_sum_kernel<OP>), dim3((unsigned)cdiv(rows * (p.ld_part / 4), 256)), dim3(256), 0, st, a);
+        GRP_LAUNCH_CHECK();
+    }
+    return GRP_OK;
+}
+
+bool aligned_to(const void* p, int32_t dtype) { return dtype == GRP_DTYPE_E4M3 || (uintptr_t)p % (dtype == GRP_DTYPE_BF16 ? 2 : 4) == 0; }
+grp_status check_sizes(const char* who, int64_t m, int32_t n, int32_t k) {
+    if (m < 0 || n < 1 || k < 1) return fail(GRP_EINVAL, "%s: M = %lld, N = %d, K = %d", who, (long long)m, n, k);
+    return GRP_OK;
+}
+
+}  // namespace
+}  // namespace grp
+
+extern "C" size_t grp_linear_workspace_bytes(int32_t kind, int64_t m, int32_t n, int32_t k, int32_t dtype) {
+    using namespace grp;
+    if (m < 0 || n < 1 || k < 1) return 0;
+    if (kind == GRP_LINEAR_FORWARD) return plan_of(dtype == GRP_DTYPE_E4M3 ? FWD_E4M3 : FWD_BF16, m, n, k).bytes;
+    if (kind == GRP_LINEAR_DX) return plan_of(GRAD_X, m, k, n).bytes;
+    if (kind == GRP_LINEAR_DW) return plan_of(GRAD_W, k, n, m).bytes;
+    return 0;
+}
+
+extern "C" grp_status grp_linear(int64_t m, int32_t n, int32_t k, const void* a, int64_t lda, const void* w, int64_t ldw, int32_t dtype,
+                                 const float* a_scale, const float* w_scale, const float* bias, int32_t act, const void* r, int64_t ldr, void* c,
+                                 int64_t ldc, int32_t c_dtype, void* z, int64_t ldz, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace grp;
+    GRP_TRY(check_sizes("grp_linear", m, n, k));
+    const bool e8 = dtype == GRP_DTYPE_E4M3;
+    if (!e8 && dtype != GRP_DTYPE_BF16) return fail(GRP_EINVAL, "grp_linear: operands are bf16 or e4m3");
+    if (c_dtype != GRP_DTYPE_FP32 && c_dtype != GRP_DTYPE_BF16) return fail(GRP_EINVAL, "grp_linear: c is fp32 or bf16");
+    if (act < GRP_ACT_NONE || act > GRP_ACT_SILU) return fail(GRP_EINVAL, "grp_linear: bad activation %d", act);
+    if (lda < k || ldw < (e8 ? k : n) || ldc < n || (r && ldr < n) || (z && ldz < n)) return fail(GRP_EINVAL, "grp_linear: a pitch is below the row's length");
+    if (!e8 && (a_scale || w_scale)) return fail(GRP_EINVAL, "grp_linear: scales belong to 8-bit operands");
+    if (m == 0) return GRP_OK;
+    if (!a || !w || !c) return fail(GRP_EINVAL, "grp_linear: null argument");
+    if (!aligned_to(a, dtype) || !aligned_to(w, dtype) || !aligned_to(c, c_dtype) || !aligned_to(r, c_dtype) || !aligned_to(z, GRP_DTYPE_BF16) ||
+        !aligned_to(bias, GRP_DTYPE_FP32) || !aligned_to(a_scale, GRP_DTYPE_FP32) || !aligned_to(w_scale, GRP_DTYPE_FP32))
+        return fail(GRP_EINVAL, "grp_linear: a pointer is not aligned to its elements");
+    LinearArgs x = {};
+    x.P = a; x.ldp = lda; x.Q = w; x.ldq = ldw; x.I = m; x.J = n; x.S = k;
+    x.a_scale = a_scale; x.w_scale = w_scale; x.bias = bias; x.act = act; x.r = r; x.ldr = ldr;
+    x.c = c; x.ldc = ldc; x.c_bf16 = c_dtype == GRP_DTYPE_BF16; x.z = z; x.ldz = ldz;
+    const double es = e8 ? 1.0 : 2.0, cs = x.c_bf16 ? 2.0 : 4.0;
+    const double bytes = ((double)m * k + (double)n * k) * es + (double)m * n * (cs * (r ? 2 : 1) + (z ? 2 : 0));
+    if (e8) return run_linear<FWD_E4M3>("grp_linear", "linear_e4m3", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+    return run_linear<FWD_BF16>("grp_linear", "linear_bf16", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+extern "C" grp_status grp_linear_dx(int64_t m, int32_t n, int32_t k, const void* dz, int64_t lddz, const void* w, int64_t ldw, int32_t act,
+                                    const void* zin, int64_t ldzin, void* da, int64_t ldda, int32_t da_dtype, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+    using namespace grp;
+    GRP_TRY(check_sizes("grp_linear_dx", m, n, k));
+    if (da_dtype != GRP_DTYPE_FP32 && da_dtype != GRP_DTYPE_BF16) return fail(GRP_EINVAL, "grp_linear_dx: da is fp32 or bf16");
+    if (act < GRP_ACT_NONE || act > GRP_ACT_SILU) return fail(GRP_EINVAL, "grp_linear_dx: bad activation %d", act);
+    const bool slope = act != GRP_ACT_NONE;
+    if (lddz < n || ldw < n || ldda < k || (slope && ldzin < k)) return fail(GRP_EINVAL, "grp_linear_dx: a pitch is below the row's length");
+    if (m == 0) return GRP_OK;
+    if (!dz || !w || !da || (slope && !zin)) return fail(GRP_EINVAL, "grp_linear_dx: null argument");
+    if (!aligned_to(dz, GRP_DTYPE_BF16) || !aligned_to(w, GRP_DTYPE_BF16) || !aligned_to(da, da_dtype) || (slope && !aligned_to(zin, GRP_DTYPE_BF16)))
+        return fail(GRP_EINVAL, "grp_linear_dx: a pointer is not aligned to its elements");
+    LinearArgs x = {};
+    x.P = dz; x.ldp = lddz; x.Q = w; x.ldq = ldw; x.I = m; x.J = k; x.S = n;
+    x.act = act; x.z = slope ? const_cast<void*>(zin) : nullptr; x.ldz = ldzin;
+    x.c = da; x.ldc = ldda; x.c_bf16 = da_dtype == GRP_DTYPE_BF16;
+    const double bytes = 2.0 * ((double)m * n + (double)k * n) + (double)m * k * ((x.c_bf16 ? 2.0 : 4.0) + (slope ? 2.0 : 0.0));
+    return run_linear<GRAD_X>("grp_linear_dx", "linear_dx", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+extern "C" grp_status grp_linear_dw(int64_t m, int32_t n, int32_t k, const void* a, int64_t lda, const void* dz, int64_t lddz, float* dw, int64_t lddw,
+                                    float* db, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace grp;
+    GRP_TRY(check_sizes("grp_linear_dw", m, n, k));
+    if (lda < k || lddz < n || lddw < n) return fail(GRP_EINVAL, "grp_linear_dw: a pitch is below the row's length");
+    if (!dw || (m > 0 && (!a || !dz))) return fail(GRP_EINVAL, "grp_linear_dw: null argument");
+    if (!aligned_to(a, GRP_DTYPE_BF16) || !aligned_to(dz, GRP_DTYPE_BF16) || !aligned_to(dw, GRP_DTYPE_FP32) || !aligned_to(db, GRP_DTYPE_FP32))
+        return fail(GRP_EINVAL, "grp_linear_dw: a pointer is not aligned to its elements");
+    LinearArgs x = {};
+    x.P = a; x.ldp = lda; x.Q = dz; x.ldq = lddz; x.I = k; x.J = n; x.S = m;
+    x.c = dw; x.ldc = lddw; x.db = db;
+    const double bytes = 2.0 * (double)m * ((double)n + k) + 4.0 * ((double)n * k + n);
+    return run_linear<GRAD_W>("grp_linear_dw", "linear_dw", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+}
