@@ -5,7 +5,8 @@
 //   dw        dW = A^T dZ,  db = column sums of dZ                                                                        sum over the rows
 //
 // The 8-bit matrix instructions cut, of every eight products, what is below 2^-13 of the largest (measured on single instructions; rms 1.3e-5 of the
-// result on normal deviates), so e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those.
+// result on normal deviates).  Beside the rounding of a bf16 result (rms 1.6e-3) that is nothing, and they run at twice the rate; for fp32 results
+// e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those.
 //
 // All are one kernel, D[i, j] = sum_s P(i, s) Q(s, j): an operand either has s contiguous ("rows": A, dZ, the 8-bit weights) or its output index
 // ("columns": W of the forward product, both operands of dw).  Products are accumulated in fp32 by the matrix unit.
@@ -27,8 +28,10 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-enum LinearOp { FWD_BF16, FWD_E4M3, GRAD_X, GRAD_W };
-constexpr int elem_size(int op) { return op == FWD_E4M3 ? 1 : 2; }
+enum LinearOp { FWD_BF16, FWD_E4M3 /* bf16 results */, FWD_E4M3_WIDE /* fp32 results */, GRAD_X, GRAD_W };
+constexpr bool is_e4m3(int op) { return op == FWD_E4M3 || op == FWD_E4M3_WIDE; }
+constexpr bool is_forward(int op) { return op == FWD_BF16 || is_e4m3(op); }
+constexpr int elem_size(int op) { return is_e4m3(op) ? 1 : 2; }
 constexpr bool p_columns(int op) { return op == GRAD_W; }
 constexpr bool q_columns(int op) { return op == GRAD_W || op == FWD_BF16; }
 
@@ -127,7 +130,7 @@ template <int OP, int N> struct ColumnTerms {
     float bias[N], ws[N];
     __device__ __forceinline__ ColumnTerms(const LinearArgs& a, int j) {
         const int n = a.J - j;
-        if constexpr (OP == FWD_BF16 || OP == FWD_E4M3) {
+        if constexpr (is_forward(OP)) {
             if (a.bias && n > 0) {
                 load_row<N>(a.bias + j, false, n, bias);
             } else {
@@ -135,7 +138,7 @@ template <int OP, int N> struct ColumnTerms {
                 for (int e = 0; e < N; ++e) bias[e] = 0.f;
             }
         }
-        if constexpr (OP == FWD_E4M3) {
+        if constexpr (is_e4m3(OP)) {
             if (a.w_scale && n > 0) {
                 load_row<N>(a.w_scale + j, false, n, ws);
             } else {
@@ -150,8 +153,8 @@ template <int OP, int N> struct ColumnTerms {
 template <int OP, int N> __device__ __forceinline__ void finish(const LinearArgs& a, int64_t i, int j, float (&v)[N], const ColumnTerms<OP, N>& col) {
     const int n = a.J - j;
     if (n <= 0) return;
-    if constexpr (OP == FWD_BF16 || OP == FWD_E4M3) {
-        if constexpr (OP == FWD_E4M3) {
+    if constexpr (is_forward(OP)) {
+        if constexpr (is_e4m3(OP)) {
             const float as = a.a_scale ? a.a_scale[i] : 1.f;
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] = v[e] * as * col.ws[e];
@@ -219,6 +222,12 @@ __device__ __forceinline__ u32x4_al load_unit(const void* base, int64_t ld, int6
     }
 }
 
+// 16 bytes a lane from buffer `rsrc` at `off` to LDS, a wavefront's 64 places in a row from byte `lds` on.  (Inline: the compiler would wait for it before
+// any other read of LDS.  No register is written; who reads the tile waits for vmcnt(0) before the barrier that is before it.)
+__device__ __forceinline__ void load_to_lds(uint32_t lds, __amdgpu_buffer_rsrc_t rsrc, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
+}
+
 // 16 e4m3 numbers in bf16 (exact).
 struct Wide8 {
     bf16x8 v[2];
@@ -237,30 +246,82 @@ struct Wide8 {
     }
 };
 
-template <int OP, int WI, int WJ, int FI> __global__ __launch_bounds__(64 * WI * WJ) void linear_kernel(LinearArgs a) {
+// Which tile a workgroup makes.  Workgroups go round the eight XCDs in turn: each of these gets a run of tiles, in bands of eight rows of tiles, so that
+// the tiles that an XCD makes at one time share their operands in its L2.
+__device__ __forceinline__ void tile_of(unsigned b, int tiles_i, int tiles_j, int& ti, int& tj) {
+    const unsigned all = (unsigned)tiles_i * (unsigned)tiles_j, xcd = b % 8, q = all / 8, r = all % 8;
+    const unsigned n = xcd * q + (xcd < r ? xcd : r) + b / 8, band = 8u * (unsigned)tiles_j;
+    const unsigned first = n / band * 8, rows = (unsigned)tiles_i - first < 8 ? (unsigned)tiles_i - first : 8, in = n % band;
+    ti = (int)(first + in % rows);
+    tj = (int)(in / rows);
+}
+
+// DMA: rows of both operands are whole units of 16 bytes and begin on them.
+template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__(64 * WI * WJ, 2) void linear_kernel(LinearArgs a) {
     constexpr int ES = elem_size(OP), NT = 64 * WI * WJ, TI = 16 * FI * WI, TJ = 64 * WJ, STEP = 128 / ES;
     constexpr bool PC = p_columns(OP), QC = q_columns(OP);
-    constexpr int UP = TI * 8 / NT, UQ = TJ * 8 / NT;
-    __shared__ __attribute__((aligned(16))) char lds[2][(TI + TJ) * 128];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, t = lane & 15;
+    constexpr int UP = TI * 8 / NT, UQ = TJ * 8 / NT, STAGE = (TI + TJ) * 128;
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, t = lane & 15;
     const int wi = wave / WJ, wj = wave % WJ;
-    const int tile = blockIdx.x % (unsigned)(a.tiles_i * a.tiles_j), split = blockIdx.x / (unsigned)(a.tiles_i * a.tiles_j);
-    const int ti = tile / a.tiles_j, tj = tile % a.tiles_j;
+    const unsigned tiles = (unsigned)(a.tiles_i * a.tiles_j), split = blockIdx.x / tiles;
+    int ti, tj;
+    tile_of(blockIdx.x % tiles, a.tiles_i, a.tiles_j, ti, tj);
     const int64_t i0 = (int64_t)ti * TI, j0 = (int64_t)tj * TJ;
     const int64_t s_begin = split * a.steps_per_split * STEP;
     const int64_t s_end = s_begin + a.steps_per_split * STEP < a.S ? s_begin + a.steps_per_split * STEP : a.S;
 
-    u32x4_al raw[UP + UQ];
-    auto request = [&](int64_t s0) {
+    // DMA: a lane's offset into the tile for each of its units, and the buffers, which begin at the tile and end with the operand (what is past the end
+    // arrives as zeros).  Else: raw registers between two steps.
+    uint32_t off[DMA ? UP + UQ : 1];
+    u32x4_al raw[DMA ? 1 : UP + UQ];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    if constexpr (DMA) {
 #pragma unroll
-        for (int n = 0; n < UP; ++n) raw[n] = load_unit<ES, PC, false, TI>(a.P, a.ldp, i0, a.I, s0, a.S, n * NT + threadIdx.x);
+        for (int n = 0; n < UP + UQ; ++n) {
+            const bool p = n < UP;
+            const int u = (p ? n : n - UP) * NT + threadIdx.x;
+            const uint32_t ld = (uint32_t)(p ? a.ldp : a.ldq) * ES;
+            const int per = p ? (PC ? TI / 8 : 8) : (QC ? TJ / 8 : 8), row = u / per;
+            const int at = p ? swizzle<PC, false, TI>(u % per, row) : swizzle<QC, true, TJ>(u % per, row);
+            off[n] = (uint32_t)row * ld + (uint32_t)at * 16;
+        }
+    }
+    auto buffer = [&](const void* base, int64_t ld, bool columns, int64_t o0, int64_t O, int64_t s0) {
+        const int64_t at = (columns ? s0 * ld + o0 : o0 * ld + s0) * ES;
+        const int64_t end = (columns ? (a.S - 1) * ld + O : (O - 1) * ld + a.S) * ES;
+        const int64_t left = end - at < 0x7FFFFFF0 ? end - at : 0x7FFFFFF0;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)base + at), 0, (int)left, 0x00020000);
+    };
+    auto request = [&](int64_t s0, int buf) {
+        if constexpr (DMA) {
+            const __amdgpu_buffer_rsrc_t P = buffer(a.P, a.ldp, PC, i0, a.I, s0), Q = buffer(a.Q, a.ldq, QC, j0, a.J, s0);
+            const bool last = s0 + STEP > a.S;                     // places of "rows" past the end of the sums: past the buffer
+            const uint32_t left = (uint32_t)((a.S - s0) * ES);
 #pragma unroll
-        for (int n = 0; n < UQ; ++n) raw[UP + n] = load_unit<ES, QC, true, TJ>(a.Q, a.ldq, j0, a.J, s0, a.S, n * NT + threadIdx.x);
+            for (int n = 0; n < UP + UQ; ++n) {
+                const bool p = n < UP;
+                uint32_t o = off[n];
+                if (last && !(p ? PC : QC)) {
+                    const int u = (p ? n : n - UP) * NT + threadIdx.x;
+                    const int at = p ? swizzle<PC, false, TI>(u & 7, u >> 3) : swizzle<QC, true, TJ>(u & 7, u >> 3);
+                    o = (uint32_t)at * 16 < left ? o : 0x80000000u;
+                }
+                load_to_lds(lds0 + buf * STAGE + ((p ? n * NT : TI * 8 + (n - UP) * NT) + wave * 64) * 16, p ? P : Q, o);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < UP; ++n) raw[n] = load_unit<ES, PC, false, TI>(a.P, a.ldp, i0, a.I, s0, a.S, n * NT + threadIdx.x);
+#pragma unroll
+            for (int n = 0; n < UQ; ++n) raw[UP + n] = load_unit<ES, QC, true, TJ>(a.Q, a.ldq, j0, a.J, s0, a.S, n * NT + threadIdx.x);
+        }
     };
     auto put = [&](int buf) {
+        if constexpr (!DMA) {
 #pragma unroll
-        for (int n = 0; n < UP + UQ; ++n)
-            *reinterpret_cast<u32x4_al*>(lds[buf] + ((n < UP ? n * NT : TI * 8 + (n - UP) * NT) + threadIdx.x) * 16) = raw[n];
+            for (int n = 0; n < UP + UQ; ++n)
+                *reinterpret_cast<u32x4_al*>(lds + buf * STAGE + ((n < UP ? n * NT : TI * 8 + (n - UP) * NT) + threadIdx.x) * 16) = raw[n];
+        }
     };
 
     floatx4 acc[FI][4], sums[4];
@@ -302,51 +363,70 @@ template <int OP, int WI, int WJ, int FI> __global__ __launch_bounds__(64 * WI *
         }
     };
 
-    if (s_begin < s_end) {
-        request(s_begin);
-        put(0);
-        int buf = 0;
-        for (int64_t s0 = s_begin; s0 < s_end; s0 += STEP, buf ^= 1) {
-            __syncthreads();
-            const bool more = s0 + STEP < s_end;
-            if (more) request(s0 + STEP);
-            const char* const L = lds[buf];
-            if constexpr (ES == 1) {
+    auto multiply = [&](const char* const L) {
+        if constexpr (OP == FWD_E4M3) {
+            intx8 q[4];
+            auto whole = [&](auto at, int f) {
+                const u32x4_al lo = *reinterpret_cast<const u32x4_al*>(L + at(f, 0, 0)), hi = *reinterpret_cast<const u32x4_al*>(L + at(f, 1, 0));
+                return __builtin_bit_cast(intx8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    Wide8 q[4];
+            for (int f = 0; f < 4; ++f) q[f] = whole(at_q, f);
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) q[f] = Wide8(*reinterpret_cast<const u32x4_al*>(L + at_q(f, s, 0)));
+            for (int i = 0; i < FI; ++i) {
+                const intx8 p = whole(at_p, i);
 #pragma unroll
-                    for (int i = 0; i < FI; ++i) {
-                        const Wide8 p(*reinterpret_cast<const u32x4_al*>(L + at_p(i, s, 0)));
+                for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q[f], p, acc[i][f], 0, 0, 0, 0, 0, 0);
+            }
+        } else if constexpr (OP == FWD_E4M3_WIDE) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+            for (int s = 0; s < 2; ++s) {
+                Wide8 q[4];
 #pragma unroll
-                            for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f].v[h], p.v[h], acc[i][f], 0, 0, 0);
-                    }
+                for (int f = 0; f < 4; ++f) q[f] = Wide8(*reinterpret_cast<const u32x4_al*>(L + at_q(f, s, 0)));
+#pragma unroll
+                for (int i = 0; i < FI; ++i) {
+                    const Wide8 p(*reinterpret_cast<const u32x4_al*>(L + at_p(i, s, 0)));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f].v[h], p.v[h], acc[i][f], 0, 0, 0);
                 }
-            } else {
+            }
+        } else {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    bf16x8 q[4];
+            for (int s = 0; s < 2; ++s) {
+                bf16x8 q[4];
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) q[f] = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, QC>(), at_q, f, s));
+                for (int f = 0; f < 4; ++f) q[f] = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, QC>(), at_q, f, s));
 #pragma unroll
-                    for (int i = 0; i < FI; ++i) {
-                        const bf16x8 p = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, PC>(), at_p, i, s));
+                for (int i = 0; i < FI; ++i) {
+                    const bf16x8 p = __builtin_bit_cast(bf16x8, read(L, std::integral_constant<bool, PC>(), at_p, i, s));
 #pragma unroll
-                        for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], p, acc[i][f], 0, 0, 0);
-                    }
-                    if constexpr (OP == GRAD_W) {
-                        if (make_sums) {
-                            const bf16x8 one = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+                    for (int f = 0; f < 4; ++f) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], p, acc[i][f], 0, 0, 0);
+                }
+                if constexpr (OP == GRAD_W) {
+                    if (make_sums) {
+                        const bf16x8 one = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-                            for (int f = 0; f < 4; ++f) sums[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], one, sums[f], 0, 0, 0);
-                        }
+                        for (int f = 0; f < 4; ++f) sums[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[f], one, sums[f], 0, 0, 0);
                     }
                 }
             }
+        }
+    };
+
+    if (s_begin < s_end) {
+        request(s_begin, 0);
+        put(0);
+        // The barrier is behind the last reads of the other stage and the arrival of this one; then the other is loaded while this one is multiplied.
+        int buf = 0;
+        for (int64_t s0 = s_begin; s0 < s_end; s0 += STEP, buf ^= 1) {
+            if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            const bool more = s0 + STEP < s_end;
+            if (more) request(s0 + STEP, buf ^ 1);
+            multiply(lds + buf * STAGE);
             if (more) put(buf ^ 1);
         }
     }
@@ -405,16 +485,20 @@ template <int OP> __global__ __launch_bounds__(256) void linear_sum_kernel(Linea
 
 // ------------------------------------------------------------------ host
 struct LinearPlan {
+    int shape = 0;                      // of LINEAR_TILES
     int64_t steps = 0, per_split = 0;
     int32_t tiles_i = 0, tiles_j = 0, splits = 1, ld_part = 0;
     size_t bytes = 0;
 };
 constexpr int64_t MOST_TILES = (int64_t)1 << 30;
+constexpr int LINEAR_TILES[][2] = {{128, 128}, {128, 256}, {256, 256}};
 
 LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     LinearPlan p;
-    p.tiles_i = (int32_t)cdiv(I, 128);
-    p.tiles_j = (int32_t)cdiv(J, 128);
+    p.shape = 0;
+    if (cdiv(I, 256) * cdiv(J, 256) >= 200) p.shape = 2;
+    p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[p.shape][0]);
+    p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[p.shape][1]);
     p.steps = cdiv(S, 128 / elem_size(op));
     const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j;
     int64_t splits = tiles < 256 ? std::min<int64_t>(cdiv(512, tiles), cdiv(p.steps, 4)) : 1;
@@ -424,6 +508,11 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     p.ld_part = (int32_t)round_up(J, 16);
     if (p.splits > 1) p.bytes = (size_t)p.splits * (size_t)(I + (op == GRAD_W ? 1 : 0)) * p.ld_part * sizeof(float);
     return p;
+}
+
+// Whether rows of n elements, `ld` apart, are whole units of 16 bytes that begin on them (and a tile's offsets fit 31 bits).
+bool whole_units(const void* p, int64_t ld, int64_t n, int es) {
+    return (uintptr_t)p % 16 == 0 && ld * es % 16 == 0 && n * es % 16 == 0 && ld * es < (1 << 22);
 }
 
 template <int OP> grp_status run_linear(const char* who, const char* name, LinearArgs a, double bytes, void* ws, size_t ws_bytes, hipStream_t st) {
@@ -437,9 +526,16 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
     a.steps_per_split = p.per_split;
     a.tiles_i = p.tiles_i;
     a.tiles_j = p.tiles_j;
+    constexpr int ES = elem_size(OP);
+    const bool dma = whole_units(a.P, a.ldp, p_columns(OP) ? a.I : a.S, ES) && whole_units(a.Q, a.ldq, q_columns(OP) ? a.J : a.S, ES);
     {
         ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
-        hipLaunchKernelGGL((linear_kernel<OP, 2, 2, 4>), dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3(256), 0, st, a);
+        auto go = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3((unsigned)threads), 0, st, a);
+        };
+        if (p.shape == 0) { if (dma) go(linear_kernel<OP, 2, 2, 4, true>, 256); else go(linear_kernel<OP, 2, 2, 4, false>, 256); }
+        else if (p.shape == 1) { if (dma) go(linear_kernel<OP, 2, 4, 4, true>, 512); else go(linear_kernel<OP, 2, 4, 4, false>, 512); }
+        else { if (dma) go(linear_kernel<OP, 2, 4, 8, true>, 512); else go(linear_kernel<OP, 2, 4, 8, false>, 512); }
         GRP_LAUNCH_CHECK();
     }
     if (p.splits > 1) {
@@ -491,7 +587,8 @@ extern "C" grp_status grp_linear(int64_t m, int32_t n, int32_t k, const void* a,
     x.c = c; x.ldc = ldc; x.c_bf16 = c_dtype == GRP_DTYPE_BF16; x.z = z; x.ldz = ldz;
     const double es = e8 ? 1.0 : 2.0, cs = x.c_bf16 ? 2.0 : 4.0;
     const double bytes = ((double)m * k + (double)n * k) * es + (double)m * n * (cs * (r ? 2 : 1) + (z ? 2 : 0));
-    if (e8) return run_linear<FWD_E4M3>("grp_linear", "linear_e4m3", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+    if (e8 && x.c_bf16) return run_linear<FWD_E4M3>("grp_linear", "linear_e4m3", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
+    if (e8) return run_linear<FWD_E4M3_WIDE>("grp_linear", "linear_e4m3_wide", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
     return run_linear<FWD_BF16>("grp_linear", "linear_bf16", x, bytes, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
