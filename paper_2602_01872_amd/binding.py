@@ -161,8 +161,14 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it (0.3 us a call instead of 2.8, of the 7.5 that a small norm took).
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _current_raw_stream is not None:
+            return _current_raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 

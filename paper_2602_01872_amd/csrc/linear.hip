@@ -16,8 +16,7 @@
 //   rows     LDS row o (output index) has 128 bytes, eight places of 16; a lane's operand of a matrix instruction is one (bf16) or two (8 bits) places
 //   columns  LDS row s has the tile's output indices; ds_read_b64_tr_b16 turns four rows of 16 around into a lane's four consecutive s
 // Places are permuted by some bits of the row (swizzle) so that the 16 lanes of a group read different banks.
-//   The instruction's rows are D's columns: lane (g, t) holds D[i + t, j + 16 g + 4 f + e], e < 4, for the wavefront's fragments f < 4, that is 16
-// consecutive columns of one row: the epilogue loads and stores 32 or 64 bytes of a row at a time straight from registers.
+//   The instruction's rows are D's columns: lane (g, t) holds D[i + t, j + 16 g + 4 f + e], e < 4, for the wavefront's fragments f < 4: 16 consecutive columns.
 #include "common.h"
 
 namespace grp {
@@ -109,7 +108,7 @@ template <class F> __device__ __forceinline__ void for_act(int act, F f) {
     }
 }
 
-// N (4 or 16) consecutive elements of which the first n exist (the others as zeros), as they lie in memory.
+// N (4, 8 or 16) consecutive elements of which the first n exist (the others as zeros), as they lie in memory.
 template <int N, bool BF16> struct RowPart {
     uint32_t w[BF16 ? N / 2 : N];
     __device__ __forceinline__ void load(const void* p, int n) {
@@ -242,14 +241,27 @@ template <bool COLUMNS, bool IS_Q, int T> __device__ __forceinline__ int swizzle
         return T >= 128 ? pos ^ (((row & 3) << 1) | (row & 8)) : pos ^ ((row & 2) | ((row >> 1) & 4));
 }
 
-// 16 bytes of which the first n elements of ES bytes exist, the rest as zeros.
-template <int ES> __device__ __forceinline__ u32x4_al load_part(const char* p, int64_t n) {
-    if (n >= 16 / ES) return (u32x4_al)*reinterpret_cast<const u32x4_b*>(p);
+// 16 bytes of a row of n elements of ES bytes from element `at` on; what is past its end as zeros.  One load, at any byte, that stays in the row: the last
+// units are read from the row's last 16 bytes and moved down.
+template <int ES> __device__ __forceinline__ u32x4_al load_part(const char* row, int64_t at, int64_t n) {
+    constexpr int V = 16 / ES;
     u32x4_al v = {0, 0, 0, 0};
+    if (n >= V) {
+        const int64_t from = at <= n - V ? at : n - V;
+        v = (u32x4_al)*reinterpret_cast<const u32x4_b*>(row + from * ES);
+        if (at > from) {
+            const int bits = at - from < V ? (int)(at - from) * ES * 8 : 128;
+            uint64_t lo = ((uint64_t)v.y << 32) | v.x, hi = ((uint64_t)v.w << 32) | v.z;
+            lo = bits >= 128 ? 0 : bits >= 64 ? hi >> (bits & 63) : (lo >> bits) | (hi << (64 - bits));
+            hi = bits >= 64 ? 0 : hi >> (bits & 63);
+            v = u32x4_al{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+        }
+        return v;
+    }
 #pragma unroll
-    for (int e = 0; e < 16 / ES; ++e)
-        if (e < n) {
-            const uint32_t x = ES == 2 ? (uint32_t)((const uint16_t*)p)[e] : (uint32_t)((const uint8_t*)p)[e];
+    for (int e = 0; e < V; ++e)
+        if (at + e < n) {
+            const uint32_t x = ES == 2 ? (uint32_t)((const uint16_t*)row)[at + e] : (uint32_t)((const uint8_t*)row)[at + e];
             v[e * ES / 4] |= x << (8 * (e * ES % 4));
         }
     return v;
@@ -260,12 +272,12 @@ template <int ES, bool COLUMNS, bool IS_Q, int T>
 __device__ __forceinline__ u32x4_al load_unit(const void* base, int64_t ld, int64_t o0, int64_t O, int64_t s0, int64_t S, int u) {
     if constexpr (!COLUMNS) {
         const int row = u >> 3, at = swizzle<COLUMNS, IS_Q, T>(u & 7, row);
-        const int64_t o = o0 + row < O ? o0 + row : O - 1, s = s0 + at * (16 / ES);      // (a row past the end: any; it is not stored)
-        return load_part<ES>((const char*)base + (o * ld + s) * ES, S - s);
+        const int64_t o = o0 + row < O ? o0 + row : O - 1;                               // (a row past the end: any; it is not stored)
+        return load_part<ES>((const char*)base + o * ld * ES, s0 + at * (16 / ES), S);
     } else {
         const int row = u / (T / 8), at = swizzle<COLUMNS, IS_Q, T>(u % (T / 8), row);
-        const int64_t s = s0 + row, o = o0 + at * 8;
-        return load_part<ES>((const char*)base + (s * ld + o) * ES, s < S ? O - o : 0);
+        const int64_t s = s0 + row < S ? s0 + row : S - 1;
+        return load_part<ES>((const char*)base + s * ld * ES, s0 + row < S ? o0 + at * 8 : O, O);
     }
 }
 
@@ -293,17 +305,33 @@ struct Wide8 {
     }
 };
 
-// Which tile a workgroup makes.  Workgroups go round the eight XCDs in turn: each of these gets a run of tiles, in bands of eight rows of tiles, so that
-// the tiles that an XCD makes at one time share their operands in its L2.
-__device__ __forceinline__ void tile_of(unsigned b, int tiles_i, int tiles_j, int& ti, int& tj) {
-    const unsigned all = (unsigned)tiles_i * (unsigned)tiles_j, xcd = b % 8, q = all / 8, r = all % 8;
-    const unsigned n = xcd * q + (xcd < r ? xcd : r) + b / 8, band = 8u * (unsigned)tiles_j;
-    const unsigned first = n / band * 8, rows = (unsigned)tiles_i - first < 8 ? (unsigned)tiles_i - first : 8, in = n % band;
+// Which tile a workgroup makes, and of which split.  Workgroups go round the eight XCDs in turn: each of these gets a run of tiles (all of one split, then
+// the next), in bands of eight rows of tiles, so that the tiles that an XCD makes at one time share their operands in its L2.
+__device__ __forceinline__ void tile_of(unsigned b, unsigned all, int tiles_i, int tiles_j, int& ti, int& tj, unsigned& split) {
+    const unsigned xcd = b % 8, q = all / 8, r = all % 8, tiles = (unsigned)tiles_i * (unsigned)tiles_j;
+    unsigned n = xcd * q + (xcd < r ? xcd : r) + b / 8;
+    split = n / tiles;
+    n %= tiles;
+    const unsigned band = 8u * (unsigned)tiles_j, first = n / band * 8, rows = (unsigned)tiles_i - first < 8 ? (unsigned)tiles_i - first : 8, in = n % band;
     ti = (int)(first + in % rows);
     tj = (int)(in / rows);
 }
 
 // DMA: rows of both operands are whole units of 16 bytes and begin on them.
+// What a lane reads of a fragment at once: all 128 bytes of s (its part: 32) for the 8-bit instruction, else half of them.
+template <int OP> using FragOf = std::conditional_t<OP == FWD_E4M3, intx8, u32x4_al>;
+template <int OP> __device__ __forceinline__ void multiply(const FragOf<OP>& q, const FragOf<OP>& p, floatx4& c) {
+    if constexpr (OP == FWD_E4M3) {
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q, p, c, 0, 0, 0, 0, 0, 0);
+    } else if constexpr (OP == FWD_E4M3_WIDE) {
+        const Wide8 qw(q), pw(p);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qw.v[h], pw.v[h], c, 0, 0, 0);
+    } else {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), c, 0, 0, 0);
+    }
+}
+
 template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__(64 * WI * WJ, 2) void linear_kernel(LinearArgs a) {
     constexpr int ES = elem_size(OP), NT = 64 * WI * WJ, TI = 16 * FI * WI, TJ = 64 * WJ, STEP = 128 / ES;
     constexpr bool PC = p_columns(OP), QC = q_columns(OP);
@@ -311,28 +339,29 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, t = lane & 15;
     const int wi = wave / WJ, wj = wave % WJ;
-    const unsigned tiles = (unsigned)(a.tiles_i * a.tiles_j), split = blockIdx.x / tiles;
     int ti, tj;
-    tile_of(blockIdx.x % tiles, a.tiles_i, a.tiles_j, ti, tj);
+    unsigned split;
+    tile_of(blockIdx.x, gridDim.x, a.tiles_i, a.tiles_j, ti, tj, split);
     const int64_t i0 = (int64_t)ti * TI, j0 = (int64_t)tj * TJ;
     const int64_t s_begin = split * a.steps_per_split * STEP;
     const int64_t s_end = s_begin + a.steps_per_split * STEP < a.S ? s_begin + a.steps_per_split * STEP : a.S;
 
-    // DMA: a lane's offset into the tile for each of its units, and the buffers, which begin at the tile and end with the operand (what is past the end
-    // arrives as zeros).  Else: raw registers between two steps.
-    uint32_t off[DMA ? UP + UQ : 1];
+    // A lane's offset into the tile for each of its units.  DMA: the buffers begin at the tile and end with the operand (what is past the end arrives as
+    // zeros).  Else: raw registers between two steps; rows past the end are the last one.
+    uint32_t off[UP + UQ];
     u32x4_al raw[DMA ? 1 : UP + UQ];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    if constexpr (DMA) {
 #pragma unroll
-        for (int n = 0; n < UP + UQ; ++n) {
-            const bool p = n < UP;
-            const int u = (p ? n : n - UP) * NT + threadIdx.x;
-            const uint32_t ld = (uint32_t)(p ? a.ldp : a.ldq) * ES;
-            const int per = p ? (PC ? TI / 8 : 8) : (QC ? TJ / 8 : 8), row = u / per;
-            const int at = p ? swizzle<PC, false, TI>(u % per, row) : swizzle<QC, true, TJ>(u % per, row);
-            off[n] = (uint32_t)row * ld + (uint32_t)at * 16;
+    for (int n = 0; n < UP + UQ; ++n) {
+        const bool p = n < UP;
+        const int u = (p ? n : n - UP) * NT + threadIdx.x, per = p ? (PC ? TI / 8 : 8) : (QC ? TJ / 8 : 8);
+        int row = u / per;
+        const int at = p ? swizzle<PC, false, TI>(u % per, row) : swizzle<QC, true, TJ>(u % per, row);
+        if (!DMA && !(p ? PC : QC)) {
+            const int64_t most = (p ? a.I - i0 : a.J - j0) - 1;
+            row = row < most ? row : (int)most;
         }
+        off[n] = (uint32_t)row * ((uint32_t)(p ? a.ldp : a.ldq) * ES) + (uint32_t)at * 16;
     }
     auto buffer = [&](const void* base, int64_t ld, bool columns, int64_t o0, int64_t O, int64_t s0) {
         const int64_t at = (columns ? s0 * ld + o0 : o0 * ld + s0) * ES;
@@ -360,14 +389,32 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
                 o = at * (16 / ES) < a.S - aim_s ? o : 0x80000000u;
             }
             load_to_lds(lds0 + buf * STAGE + ((p ? n * NT : TI * 8 + (n - UP) * NT) + wave * 64) * 16, p ? rsrc_p : rsrc_q, o);
-        } else {
-            raw[n] = p ? load_unit<ES, PC, false, TI>(a.P, a.ldp, i0, a.I, aim_s, a.S, u) : load_unit<ES, QC, true, TJ>(a.Q, a.ldq, j0, a.J, aim_s, a.S, u);
         }
     };
     auto pieces = [&](int from, int to, int buf) {
+        if constexpr (DMA) {
 #pragma unroll
-        for (int n = 0; n < UP + UQ; ++n)
-            if (n >= from && n < to) piece(n, buf);
+            for (int n = 0; n < UP + UQ; ++n)
+                if (n >= from && n < to) piece(n, buf);
+        } else {                                                   // all at once
+            const bool inside = aim_s + STEP <= a.S;               // no unit reaches past the end of a row
+            if (inside && (!PC || i0 + TI <= a.I) && a.ldp < ((int64_t)1 << 23)) {
+                const char* base = (const char*)a.P + (PC ? aim_s * a.ldp + i0 : i0 * a.ldp + aim_s) * ES;
+#pragma unroll
+                for (int n = 0; n < UP; ++n) raw[n] = (u32x4_al)*reinterpret_cast<const u32x4_b*>(base + off[n]);
+            } else {
+#pragma unroll
+                for (int n = 0; n < UP; ++n) raw[n] = load_unit<ES, PC, false, TI>(a.P, a.ldp, i0, a.I, aim_s, a.S, n * NT + threadIdx.x);
+            }
+            if (inside && (!QC || j0 + TJ <= a.J) && a.ldq < ((int64_t)1 << 23)) {
+                const char* base = (const char*)a.Q + (QC ? aim_s * a.ldq + j0 : j0 * a.ldq + aim_s) * ES;
+#pragma unroll
+                for (int n = 0; n < UQ; ++n) raw[UP + n] = (u32x4_al)*reinterpret_cast<const u32x4_b*>(base + off[UP + n]);
+            } else {
+#pragma unroll
+                for (int n = 0; n < UQ; ++n) raw[UP + n] = load_unit<ES, QC, true, TJ>(a.Q, a.ldq, j0, a.J, aim_s, a.S, n * NT + threadIdx.x);
+            }
+        }
     };
     auto put = [&](int buf) {
         if constexpr (!DMA) {
@@ -405,8 +452,7 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
             return TI * 128 + row * 128 + 16 * swizzle<QC, true, TJ>(4 * s + g, row);
         }
     };
-    // What a lane reads of a fragment at once, and how many times a step has that: all 128 bytes of s for the 8-bit instruction, else half of them.
-    typedef std::conditional_t<OP == FWD_E4M3, intx8, u32x4_al> Frag;
+    typedef FragOf<OP> Frag;
     constexpr int PHASES = OP == FWD_E4M3 ? 1 : 2;
     auto read = [&](const char* buf, auto columns, auto at, int f, int s) -> Frag {
         if constexpr (OP == FWD_E4M3) {
@@ -423,31 +469,21 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
     };
     auto read_p = [&](const char* buf, int s, int i) { return read(buf, std::integral_constant<bool, PC>(), at_p, i, s); };
     auto read_q = [&](const char* buf, int s, int f) { return read(buf, std::integral_constant<bool, QC>(), at_q, f, s); };
-    auto multiply = [&](const Frag& q, const Frag& p, floatx4& c) {
-        if constexpr (OP == FWD_E4M3) {
-            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q, p, c, 0, 0, 0, 0, 0, 0);
-        } else if constexpr (OP == FWD_E4M3_WIDE) {
-            const Wide8 qw(q), pw(p);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qw.v[h], pw.v[h], c, 0, 0, 0);
-        } else {
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), c, 0, 0, 0);
-        }
-    };
-
     if (s_begin < s_end) {
         // A step's last TAIL rows of fragments are multiplied behind the barrier that gives its stage free, column by column; a column's operand of the next
         // step is read as soon as it is no longer needed.  So neither the barrier nor the latency of LDS leaves the matrix unit without work.
         //   The loads of the step after the next go between the products, EARLY of them behind the barrier and the others among the next step's first rows: a
-        // wavefront that asks for all of them at once is held up until the address unit has taken the 64 KB that all eight ask for.
-        constexpr int TAIL = FI > 4 ? 3 : 2, ALL = UP + UQ, EARLY = ALL / 2;
+        // wavefront that asks for all of them at once is held up until the address unit has taken the 64 KB that all eight ask for.  (8192^3, us, all at once /
+        // spread: dx 865 / 843, forward 871 / 804, dw 892 / 822, e4m3 420 / 393; of these a quarter, a half, three quarters behind the barrier: dx 859, 822,
+        // 829, e4m3 405, 409, 384.)  A wavefront that has its operands goes before one that asks for some: dx 822 -> 798.
+        constexpr int TAIL = FI > 4 ? 3 : 2, ALL = UP + UQ, EARLY = OP == FWD_E4M3 ? ALL * 3 / 4 : ALL / 2;
         Frag q[4], p[4];
         aim(s_begin);
         pieces(0, ALL, 0);
         put(0);
         aim(s_begin + STEP);
         if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        pieces(0, DMA ? EARLY : ALL, 1);
+        if (DMA || s_begin + STEP < s_end) pieces(0, DMA ? EARLY : ALL, 1);
         __syncthreads();
 #pragma unroll
         for (int f = 0; f < 4; ++f) q[f] = read_q(lds, 0, f);
@@ -462,8 +498,10 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
                     constexpr int ROWS = FI - TAIL, MORE = ALL - EARLY, EACH = (MORE + ROWS - 1) / ROWS;
                     p[(i + 1) % 4] = read_p(here, s, i + 1);
                     if (DMA && s == 0) pieces(EARLY + i * EACH, EARLY + (i + 1) * EACH, buf ^ 1);
+                    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) multiply(q[f], p[i % 4], acc[i][f]);
+                    for (int f = 0; f < 4; ++f) multiply<OP>(q[f], p[i % 4], acc[i][f]);
+                    __builtin_amdgcn_s_setprio(0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
@@ -483,11 +521,11 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
                 for (int f = 0; f < 4; ++f) {
                     if (DMA && ends) pieces(f * EARLY / 4, (f + 1) * EARLY / 4, buf);
 #pragma unroll
-                    for (int i = FI - TAIL; i < FI; ++i) multiply(q[f], p[i % 4], acc[i][f]);
+                    for (int i = FI - TAIL; i < FI; ++i) multiply<OP>(q[f], p[i % 4], acc[i][f]);
                     if constexpr (OP == GRAD_W) {
                         if (make_sums) {
                             const bf16x8 one = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-                            multiply(q[f], __builtin_bit_cast(u32x4_al, one), sums[f]);
+                            multiply<OP>(q[f], __builtin_bit_cast(u32x4_al, one), sums[f]);
                         }
                     }
                     q[f] = read_q(then, then_s, f);
@@ -498,54 +536,90 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
         if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // (no load may write LDS when it is another workgroup's)
     }
 
-    const int j = (int)j0 + wj * 64 + g * 16;
-    if (j >= a.J) return;
+    // Out by way of LDS, 32 rows of the wavefront's 64 columns at a time, in its own part of it: a wavefront then loads and stores whole lines (128 bytes of
+    // eight rows, or 256 of four).  Straight from the registers, 64 bytes of 16 rows at a time, fp32 results of 65536 x 4096 (K = 256) took 419 us, now 297.
+    __syncthreads();
+    constexpr int PITCH = 68, BATCHES = FI / 2;
+    static_assert(2 * STAGE / (WI * WJ) >= 32 * PITCH * 4, "32 rows of every wavefront fit LDS");
+    float* const mine = (float*)(lds + wave * (2 * STAGE / (WI * WJ)));
+    const int64_t row0 = i0 + wi * FI * 16;
+    const int col0 = (int)j0 + wj * 64;
+    auto batch = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(mine + (16 * i + t) * PITCH + 16 * g + 4 * f) = acc[2 * b + i][f];
+    };
+    // unit u of a batch: N columns a lane of 64 N / 64 rows
+    auto unit = [&](auto n, int u, float (&v)[decltype(n)::value]) {
+        constexpr int N = decltype(n)::value;
+        const float* p = mine + (u * N + lane / (64 / N)) * PITCH + lane % (64 / N) * N;
+#pragma unroll
+        for (int k = 0; k < N; k += 4) {
+            const floatx4 x = *reinterpret_cast<const floatx4*>(p + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[k + e] = x[e];
+        }
+    };
     if (a.splits > 1) {
         const int64_t rows = a.I + (OP == GRAD_W ? 1 : 0);
         float* const part = a.part + (int64_t)split * rows * a.ld_part;
+        const int col = col0 + lane % 16 * 4;
 #pragma unroll
-        for (int i = 0; i < FI; ++i) {
-            const int64_t row = i0 + (wi * FI + i) * 16 + t;
-            if (row < a.I)
+        for (int b = 0; b < BATCHES; ++b) {
+            batch(b);
 #pragma unroll
-                for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + row * a.ld_part + j + 4 * f) = acc[i][f];
+            for (int u = 0; u < 8; ++u) {
+                float v[4];
+                unit(std::integral_constant<int, 4>(), u, v);
+                const int64_t row = row0 + 32 * b + 4 * u + lane / 16;
+                if (row < a.I && col < a.ld_part) *reinterpret_cast<floatx4*>(part + row * a.ld_part + col) = floatx4{v[0], v[1], v[2], v[3]};
+            }
         }
-        if (OP == GRAD_W && make_sums && t == 0)
+        if (OP == GRAD_W && make_sums && t == 0 && col0 + 16 * g < a.ld_part)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + a.I * a.ld_part + j + 4 * f) = sums[f];
+            for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + a.I * a.ld_part + col0 + 16 * g + 4 * f) = sums[f];
         return;
     }
-    const ColumnTerms<OP, 16> col(a, j);
     for_more_type<OP>(a, [&](auto type) {
         constexpr bool BF16 = decltype(type)::value;
-        constexpr int ROWS = OP == GRAD_X ? FI : BF16 ? 4 : 2;            // whose further terms are on their way at once: as many as registers are left for
+        constexpr int N = BF16 ? 8 : 4, UNITS = 32 / N;
+        constexpr int AHEAD = !BF16 ? 1 : OP == GRAD_X ? BATCHES : BATCHES < 2 ? BATCHES : 2;      // batches whose further terms are on their way: what registers allow
         const bool more = takes_more<OP>(a);
+        const int col = col0 + lane % (64 / N) * N;
+        const ColumnTerms<OP, N> terms(a, col);
+        RowPart<N, BF16> further[AHEAD][UNITS];
+        auto ask = [&](int b) {
+            if (more && col < a.J)
 #pragma unroll
-        for (int first = 0; first < FI; first += ROWS) {
-            RowPart<16, BF16> terms[ROWS];
-            if (more)
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) {
-                    const int64_t row = i0 + (wi * FI + first + i) * 16 + t;
-                    if (row < a.I) load_more<OP>(a, row, j, terms[i]);
+                for (int u = 0; u < UNITS; ++u) {
+                    const int64_t row = row0 + 32 * b + u * N + lane / (64 / N);
+                    if (row < a.I) load_more<OP>(a, row, col, further[b % AHEAD][u]);
                 }
+        };
+#pragma unroll
+        for (int b = 0; b < AHEAD; ++b) ask(b);
+#pragma unroll
+        for (int b = 0; b < BATCHES; ++b) {
+            batch(b);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                const int64_t row = i0 + (wi * FI + first + i) * 16 + t;
-                float v[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = acc[first + i][e >> 2][e & 3];
-                if (row < a.I) finish<OP, 16, BF16>(a, row, j, v, col, more, terms[i]);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int u = 0; u < UNITS; ++u) {
+                float v[N];
+                unit(std::integral_constant<int, N>(), u, v);
+                const int64_t row = row0 + 32 * b + u * N + lane / (64 / N);
+                if (row < a.I) finish<OP, N, BF16>(a, row, col, v, terms, more, further[b % AHEAD][u]);
             }
+            if (b + AHEAD < BATCHES) ask(b + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
         }
     });
     if (OP == GRAD_W && make_sums && t == 0) {
         float v[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = sums[e >> 2][e & 3];
-        store_row<16, false>(a.db + j, a.J - j, v);
+        const int col = col0 + 16 * g;
+        if (col < a.J) store_row<16, false>(a.db + col, a.J - col, v);
     }
 }
 
@@ -572,28 +646,186 @@ template <int OP> __global__ __launch_bounds__(256) void linear_sum_kernel(Linea
     });
 }
 
+// ------------------------------------------------------------------ few rows
+// Products of at most 64 rows are bound by reading W once.  A workgroup of sixteen wavefronts makes 16 MI rows and 32 columns; every wavefront takes blocks of
+// 128 bytes of s (all sixteen together consecutive ones) straight into registers, several in flight, and the sixteen sums are added in LDS: one
+// launch, however long the sums.  W by columns: a lane loads two columns of eight rows and turns them around with eight byte permutations.
+//   Lane (g, t) has D[t, 8 g + 2 e + f]: fragment f holds the columns 2 t + f.
+template <int OP> struct FewBlock {                    // a lane's part of 128 bytes of s
+    static constexpr int ES = elem_size(OP), STEP = 128 / ES;
+    static constexpr bool QC = q_columns(OP);
+    u32x4_al q[QC ? 1 : 4];                            // rows: fragment f's halves at 2 f, 2 f + 1
+    uint32_t c[QC ? 16 : 1];                           // columns: two of row 32 s + 8 g + k at 8 s + k
+
+    // jc: the lane's columns (QC: two of J >= 2, from jc on) / rows of Q (jr[2]), all existing
+    __device__ __forceinline__ void load(const LinearArgs& a, int64_t s0, int g, int64_t jc, const int64_t (&jr)[2], bool whole) {
+        if constexpr (QC) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int64_t s = s0 + (k >> 3) * 32 + 8 * g + (k & 7);
+                c[k] = 0;
+                if (whole || s < a.S) c[k] = *reinterpret_cast<const u32_any*>((const uint16_t*)a.Q + s * a.ldq + jc);
+            }
+        } else {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) q[2 * f + h] = part_of(a.Q, a.ldq, jr[f], s0, a.S, 4 * h + g, whole);
+        }
+    }
+    static __device__ __forceinline__ u32x4_al part_of(const void* base, int64_t ld, int64_t o, int64_t s0, int64_t S, int at, bool whole) {
+        const int64_t s = s0 + at * (16 / ES);
+        const char* row = (const char*)base + o * ld * ES;
+        if (whole) return (u32x4_al)*reinterpret_cast<const u32x4_b*>(row + s * ES);
+        return load_part<ES>(row, s, S);
+    }
+    // fragment f's operand of half h (bf16 instructions)
+    __device__ __forceinline__ u32x4_al operand(int f, int h, int shift) const {
+        if constexpr (!QC) return q[2 * f + h];
+        u32x4_al v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = c[8 * h + 2 * k] >> shift, hi = c[8 * h + 2 * k + 1] >> shift;
+            v[k] = __builtin_amdgcn_perm(hi, lo, f ? 0x07060302u : 0x05040100u);
+        }
+        return v;
+    }
+};
+
+constexpr int FEW_WAVES = 16;
+template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a) {
+    typedef FewBlock<OP> Block;
+    constexpr int STEP = Block::STEP, U = MI == 1 ? 4 : MI == 2 ? 2 : 1;
+    __shared__ float part[FEW_WAVES][16 * MI][36];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, t = lane & 15;
+    // workgroups b and b + 8 run on one XCD: they share the lines of W's rows
+    const unsigned nb = (unsigned)a.tiles_j, b = blockIdx.x, pairs = nb / 16 * 16;
+    const unsigned col_block = b < pairs ? b / 16 * 16 + (b % 8) * 2 + (b / 8) % 2 : b;
+    const int64_t j0 = (int64_t)col_block * 32, i0 = (int64_t)blockIdx.y * 16 * MI;
+    const int64_t j = j0 + 2 * t, jc = j + 1 < a.J ? j : a.J - 2;
+    const int shift = j - jc == 1 ? 16 : 0;                                      // (the last column of an odd number; columns past the end: any)
+    const int64_t jr[2] = {j < a.J ? j : a.J - 1, j + 1 < a.J ? j + 1 : a.J - 1};
+    int64_t row[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) row[i] = i0 + 16 * i + t < a.I ? i0 + 16 * i + t : a.I - 1;
+
+    floatx4 acc[MI][2];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) acc[i][0] = acc[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto take = [&](auto count, int64_t s0, bool whole) {
+        constexpr int N = decltype(count)::value;
+        Block q[N];
+        u32x4_al p[N][MI][2];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            q[n].load(a, s0 + n * STEP, g, jc, jr, whole);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) p[n][i][h] = Block::part_of(a.P, a.ldp, row[i], s0 + n * STEP, a.S, 4 * h + g, whole);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                if constexpr (OP == FWD_E4M3) {
+                    const intx8 w = __builtin_bit_cast(intx8, __builtin_shufflevector(q[n].q[2 * f], q[n].q[2 * f + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+                        multiply<OP>(w, __builtin_bit_cast(intx8, __builtin_shufflevector(p[n][i][0], p[n][i][1], 0, 1, 2, 3, 4, 5, 6, 7)), acc[i][f]);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const u32x4_al w = q[n].operand(f, h, shift);
+#pragma unroll
+                        for (int i = 0; i < MI; ++i) multiply<OP>(w, p[n][i][h], acc[i][f]);
+                    }
+                }
+            }
+    };
+    const int64_t full = a.S / STEP;
+    int64_t k = (int64_t)wave * U;
+    for (; k + U <= full; k += FEW_WAVES * U) take(std::integral_constant<int, U>(), k * STEP, true);
+    for (int64_t end = k + U; k < end && k * STEP < a.S; ++k) take(std::integral_constant<int, 1>(), k * STEP, k < full);
+
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) part[wave][16 * i + t][8 * g + 2 * e + f] = acc[i][f][e];
+    __syncthreads();
+    const int r = threadIdx.x / 8, c4 = threadIdx.x % 8 * 4;
+    if (r >= 16 * MI || i0 + r >= a.I || j0 + c4 >= a.J) return;
+    floatx4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) s += *reinterpret_cast<const floatx4*>(&part[w][r][c4]);
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    for_more_type<OP>(a, [&](auto type) {
+        RowPart<4, decltype(type)::value> terms;
+        const bool more = takes_more<OP>(a);
+        if (more) load_more<OP>(a, i0 + r, (int)j0 + c4, terms);
+        finish<OP, 4, decltype(type)::value>(a, i0 + r, (int)j0 + c4, v, ColumnTerms<OP, 4>(a, (int)j0 + c4), more, terms);
+    });
+}
+
 // ------------------------------------------------------------------ host
 struct LinearPlan {
     int shape = 0;                      // of LINEAR_TILES
+    int few = 0;                        // fragments of rows of linear_few_kernel (0: tiles)
     int64_t steps = 0, per_split = 0;
     int32_t tiles_i = 0, tiles_j = 0, splits = 1, ld_part = 0;
     size_t bytes = 0;
 };
 constexpr int64_t MOST_TILES = (int64_t)1 << 30;
-constexpr int LINEAR_TILES[][2] = {{128, 128}, {128, 256}, {256, 256}};
+// The tiles there are, and what a step of 128 bytes of one takes, in us, with one workgroup on a CU and with as many as fit there; what a tile takes
+// besides (measured on products of K = 64 .. 4096 over 128 .. 3e5 rows).
+struct TileShape { int i, j, most, threads; float step[3], besides; };
+constexpr TileShape LINEAR_TILES[] = {{64, 128, 3, 128, {0.50f, 0.55f, 0.78f}, 1.5f}, {128, 128, 2, 256, {0.62f, 0.95f, 0.f}, 2.f}, {256, 256, 1, 512, {1.6f, 0.f, 0.f}, 6.f}};
+constexpr int CUS = 256;
 
+// The tile and the number of splits of the sums with the least time by a model of it: workgroups in rounds of what fits the CUs, 15 TB/s for the tiles' loads,
+// and for splits a second launch (3.5 us, with what the host takes for it) that reads the partial sums.  Against the best of all tiles and splits, on 90
+// products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 12 % at most, dw 2.6 % and 26 %.  Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096,
+// K = 4096: 256 x 256 211, 128 x 128 258; 512 x 256, K = 256: 64 x 128 8.0, 256 x 256 15.8; dw over 8192 rows, 256 x 256: 64 x 128 in 16 splits 14.6, unsplit 81.
 LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     LinearPlan p;
-    p.shape = 0;
-    if (cdiv(I, 256) * cdiv(J, 256) >= 200) p.shape = 2;
-    p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[p.shape][0]);
-    p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[p.shape][1]);
-    p.steps = cdiv(S, 128 / elem_size(op));
-    const int64_t tiles = (int64_t)p.tiles_i * p.tiles_j;
-    int64_t splits = tiles < 256 ? std::min<int64_t>(cdiv(512, tiles), cdiv(p.steps, 4)) : 1;
-    if (splits < 1) splits = 1;
-    p.per_split = std::max<int64_t>(1, cdiv(p.steps, splits));
-    p.splits = (int32_t)std::max<int64_t>(1, cdiv(p.steps, p.per_split));
+    p.steps = std::max<int64_t>(1, cdiv(S, 128 / elem_size(op)));
+    const int64_t s_bytes = S * elem_size(op);
+    // Few rows: one launch, as long as the sums are not so long that the CUs without a workgroup would have halved the time.  Forward of bf16, J = 4096, us, this and
+    // tiles: 1 row, K = 2048 7.5 and 9.1, K = 4096 14.1 and 11.0; 32 rows, K = 2048 8.3 and 12.1; 64 rows, K = 1024 8.2 and 12.6, K = 2048 (J = 256) 11.3 and 11.1.
+    if (op != GRAD_W && I <= 64 && J >= 2 && s_bytes <= (I <= 32 ? 6144 : 3072)) {
+        p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
+        p.tiles_j = (int32_t)cdiv(J, 32);
+        return p;
+    }
+    double best = 0.0;
+    const double extra = op == GRAD_W ? 1.0 : 0.0;
+    for (int shape = 0; shape < 3; ++shape) {
+        const TileShape& t = LINEAR_TILES[shape];
+        const double tiles = (double)cdiv(I, t.i) * (double)cdiv(J, t.j);
+        for (int64_t splits = 1; splits <= p.steps && splits <= 512 && (splits == 1 || tiles * splits <= 16.0 * CUS); splits *= 2) {
+            const int64_t per = cdiv(p.steps, splits), real = cdiv(p.steps, per);
+            const double work = tiles * real;
+            double rounds = 1.0;
+            int on = (int)std::min<double>(t.most, ceil(work / CUS));
+            if (work > (double)CUS * t.most) {
+                rounds = work / ((double)CUS * t.most);
+                rounds = rounds < 4.0 ? ceil(rounds) : rounds + 0.5;
+            }
+            double us = 3.5 + std::max(rounds * (per * (double)t.step[on - 1] + t.besides * (0.5 + 0.5 * on)), work * per * (t.i + t.j) * 128.0 / 15e6);
+            if (real > 1) us += 3.5 + ((double)I + extra) * J * 4.0 * real / 2.5e6 + 0.02 * real;
+            if (best == 0.0 || us < best) {
+                best = us;
+                p.shape = shape;
+                p.per_split = per;
+                p.splits = (int32_t)real;
+            }
+        }
+    }
+    p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[p.shape].i);
+    p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[p.shape].j);
     p.ld_part = (int32_t)round_up(J, 16);
     if (p.splits > 1) p.bytes = (size_t)p.splits * (size_t)(I + (op == GRAD_W ? 1 : 0)) * p.ld_part * sizeof(float);
     return p;
@@ -615,16 +847,26 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
     a.steps_per_split = p.per_split;
     a.tiles_i = p.tiles_i;
     a.tiles_j = p.tiles_j;
+    if constexpr (OP != GRAD_W)
+        if (p.few) {
+            ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_j, (unsigned)cdiv(a.I, 16 * p.few)), dim3(64 * FEW_WAVES), 0, st, a); };
+            if (p.few == 1) go(linear_few_kernel<OP, 1>);
+            else if (p.few == 2) go(linear_few_kernel<OP, 2>);
+            else go(linear_few_kernel<OP, 4>);
+            GRP_LAUNCH_CHECK();
+            return GRP_OK;
+        }
     constexpr int ES = elem_size(OP);
     const bool dma = whole_units(a.P, a.ldp, p_columns(OP) ? a.I : a.S, ES) && whole_units(a.Q, a.ldq, q_columns(OP) ? a.J : a.S, ES);
     {
         ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
-        auto go = [&](auto kernel, int threads) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3((unsigned)threads), 0, st, a);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3((unsigned)LINEAR_TILES[p.shape].threads), 0, st, a);
         };
-        if (p.shape == 0) { if (dma) go(linear_kernel<OP, 2, 2, 4, true>, 256); else go(linear_kernel<OP, 2, 2, 4, false>, 256); }
-        else if (p.shape == 1) { if (dma) go(linear_kernel<OP, 2, 4, 4, true>, 512); else go(linear_kernel<OP, 2, 4, 4, false>, 512); }
-        else { if (dma) go(linear_kernel<OP, 2, 4, 8, true>, 512); else go(linear_kernel<OP, 2, 4, 8, false>, 512); }
+        if (p.shape == 0) { if (dma) go(linear_kernel<OP, 1, 2, 4, true>); else go(linear_kernel<OP, 1, 2, 4, false>); }
+        else if (p.shape == 1) { if (dma) go(linear_kernel<OP, 2, 2, 4, true>); else go(linear_kernel<OP, 2, 2, 4, false>); }
+        else { if (dma) go(linear_kernel<OP, 2, 4, 8, true>); else go(linear_kernel<OP, 2, 4, 8, false>); }
         GRP_LAUNCH_CHECK();
     }
     if (p.splits > 1) {
