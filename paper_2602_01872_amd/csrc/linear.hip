@@ -39,6 +39,7 @@ struct LinearArgs {
     int64_t ldp;
     const void* Q;
     int64_t ldq;
+    int64_t end_p, end_q;             // bytes of the operands, to the end of their last rows
     int64_t I, S;                     // rows of D, length of the sums
     int32_t J;                        // columns of D
     const float *a_scale, *w_scale, *bias;
@@ -168,6 +169,7 @@ template <int N, bool BF16> __device__ __forceinline__ void store_row(void* p, i
 // What depends on the columns alone.
 template <int OP, int N> struct ColumnTerms {
     RowPart<N, false> bias, ws;
+    ColumnTerms() = default;
     __device__ __forceinline__ ColumnTerms(const LinearArgs& a, int j) {
         const int n = a.J - j;
         if constexpr (is_forward(OP)) bias.load(a.bias + j, a.bias ? n : 0);
@@ -241,6 +243,41 @@ template <bool COLUMNS, bool IS_Q, int T> __device__ __forceinline__ int swizzle
         return T >= 128 ? pos ^ (((row & 3) << 1) | (row & 8)) : pos ^ ((row & 2) | ((row >> 1) & 4));
 }
 
+// v moved down by some elements of ES bytes, zeros above them.
+template <int ES> __device__ __forceinline__ u32x4_al moved_down(u32x4_al v, int64_t elements) {
+    const int bits = elements < 16 / ES ? (int)elements * ES * 8 : 128;
+    uint64_t lo = ((uint64_t)v.y << 32) | v.x, hi = ((uint64_t)v.w << 32) | v.z;
+    if (bits > 0) {
+        lo = bits >= 128 ? 0 : bits >= 64 ? hi >> (bits & 63) : (lo >> bits) | (hi << (64 - bits));
+        hi = bits >= 64 ? 0 : hi >> bits;
+    }
+    return u32x4_al{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+// 16 bytes from any byte on, by loads of whole dwords and a shift at the end: 16 bytes a lane at 2-byte boundaries take the address unit more than twice
+// as long as at 4-byte ones (3e5 x 65 by 65 x 65 63 us, 66 x 66 33).  Each dword that is read holds some of the 16 bytes.
+struct AnyUnit {
+    u32x4_al x;
+    uint32_t y, shift;
+    __device__ __forceinline__ void load(const char* p) {
+        const uint32_t m = (uint32_t)(uintptr_t)p & 3;
+        const char* const at = p - m;
+        typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+        x = (u32x4_al)*reinterpret_cast<const u32x4_4*>(at);
+        y = *reinterpret_cast<const uint32_t*>(at + (m ? 16 : 12));
+        shift = m * 8;
+    }
+    __device__ __forceinline__ u32x4_al value() const {
+        return u32x4_al{__builtin_amdgcn_alignbit(x.y, x.x, shift), __builtin_amdgcn_alignbit(x.z, x.y, shift), __builtin_amdgcn_alignbit(x.w, x.z, shift),
+                        __builtin_amdgcn_alignbit(y, x.w, shift)};
+    }
+};
+
+struct PlainUnit {
+    u32x4_al x;
+    __device__ __forceinline__ void load(const char* p) { x = (u32x4_al)*reinterpret_cast<const u32x4_b*>(p); }
+    __device__ __forceinline__ u32x4_al value() const { return x; }
+};
+
 // 16 bytes of a row of n elements of ES bytes from element `at` on; what is past its end as zeros.  One load, at any byte, that stays in the row: the last
 // units are read from the row's last 16 bytes and moved down.
 template <int ES> __device__ __forceinline__ u32x4_al load_part(const char* row, int64_t at, int64_t n) {
@@ -249,14 +286,7 @@ template <int ES> __device__ __forceinline__ u32x4_al load_part(const char* row,
     if (n >= V) {
         const int64_t from = at <= n - V ? at : n - V;
         v = (u32x4_al)*reinterpret_cast<const u32x4_b*>(row + from * ES);
-        if (at > from) {
-            const int bits = at - from < V ? (int)(at - from) * ES * 8 : 128;
-            uint64_t lo = ((uint64_t)v.y << 32) | v.x, hi = ((uint64_t)v.w << 32) | v.z;
-            lo = bits >= 128 ? 0 : bits >= 64 ? hi >> (bits & 63) : (lo >> bits) | (hi << (64 - bits));
-            hi = bits >= 64 ? 0 : hi >> (bits & 63);
-            v = u32x4_al{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-        }
-        return v;
+        return at > from ? moved_down<ES>(v, at - from) : v;
     }
 #pragma unroll
     for (int e = 0; e < V; ++e)
@@ -363,9 +393,8 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
         }
         off[n] = (uint32_t)row * ((uint32_t)(p ? a.ldp : a.ldq) * ES) + (uint32_t)at * 16;
     }
-    auto buffer = [&](const void* base, int64_t ld, bool columns, int64_t o0, int64_t O, int64_t s0) {
+    auto buffer = [&](const void* base, int64_t ld, bool columns, int64_t o0, int64_t end, int64_t s0) {
         const int64_t at = (columns ? s0 * ld + o0 : o0 * ld + s0) * ES;
-        const int64_t end = (columns ? (a.S - 1) * ld + O : (O - 1) * ld + a.S) * ES;
         const int64_t left = s0 >= s_end ? 0 : end - at < 0x7FFFFFF0 ? end - at : 0x7FFFFFF0;
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)base + at), 0, (int)left, 0x00020000);
     };
@@ -375,8 +404,8 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
     auto aim = [&](int64_t s0) {
         aim_s = s0;
         if constexpr (DMA) {
-            rsrc_p = buffer(a.P, a.ldp, PC, i0, a.I, s0);
-            rsrc_q = buffer(a.Q, a.ldq, QC, j0, a.J, s0);
+            rsrc_p = buffer(a.P, a.ldp, PC, i0, a.end_p, s0);
+            rsrc_q = buffer(a.Q, a.ldq, QC, j0, a.end_q, s0);
         }
     };
     auto piece = [&](int n, int buf) {
@@ -770,10 +799,152 @@ template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void line
     });
 }
 
+// ------------------------------------------------------------------ many rows, short sums
+// Products of many rows with sums of at most 1024 bytes are bound by their rows, not by arithmetic, and in tiles a workgroup mostly waits: for its first loads,
+// for its last stores.  Here W stays: a workgroup keeps up to 128 KB of it (blocks of 64 columns) in LDS, and each of its eight wavefronts walks over rows, 16 at a
+// time, on its own: their 16 x S operands come straight into registers, one walk ahead, no barrier in the loop, and 64 columns after the other are
+// multiplied and stored.  Over 3e5 rows, us, tiles and this: 64 by 64 35 and 21, K = 256 by 47 102 and 61; 256 by 256 139 and 150.  It takes rows at any
+// alignment (ODD: that are no whole dwords): 65 by 65 63 and 48; 8192 rows of them 12.9 and 7.6.
+//   CHUNKS: of 64 bytes of s; BLOCKS: of 64 columns that LDS has room for at CHUNKS.  fp32 results: fragment f has columns 16 f + t, so that a store has 64
+// bytes of a row; bf16: lane g has 16 columns, 32 bytes of its row.
+constexpr int TALL_WAVES = 8;
+template <int OP, int CHUNKS, bool CF32, bool ODD, int LDS_KB> __global__ __launch_bounds__(64 * TALL_WAVES, 2) void linear_tall_kernel(LinearArgs a, int blocks, int64_t rows_16) {
+    static_assert(OP == FWD_BF16 || OP == GRAD_X, "bf16 operands");
+    constexpr bool QC = q_columns(OP);
+    constexpr int STEPS = (CHUNKS + 1) / 2, BLOCK = STEPS * 64 * 128, BLOCKS = LDS_KB * 1024 / BLOCK;
+    __shared__ __attribute__((aligned(16))) char lds[BLOCKS * BLOCK];
+    __shared__ float lds_bias[BLOCKS * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, t = lane & 15;
+    const int64_t j0 = (int64_t)blockIdx.y * blocks * 64;
+    const int mine = (int)((a.J - j0 + 63) / 64) < blocks ? (int)((a.J - j0 + 63) / 64) : blocks;
+
+    for (int u = threadIdx.x; u < mine * (BLOCK / 16); u += 64 * TALL_WAVES) {
+        const int b = u / (BLOCK / 16), step = u % (BLOCK / 16) / 512;
+        *reinterpret_cast<u32x4_al*>(lds + u * 16) = load_unit<2, QC, !CF32, 64>(a.Q, a.ldq, j0 + b * 64, a.J, step * 64, a.S, u % 512);
+    }
+    if constexpr (OP == FWD_BF16)
+        for (int c = threadIdx.x; c < mine * 64; c += 64 * TALL_WAVES) lds_bias[c] = a.bias && j0 + c < a.J ? a.bias[j0 + c] : 0.f;
+    __syncthreads();
+
+    auto operand = [&](int b, int f, int chunk) -> bf16x8 {
+        const char* const L = lds + b * BLOCK + (chunk >> 1) * (64 * 128);
+        const int s = chunk & 1;
+        if constexpr (QC) {
+            typedef shortx4 __attribute__((address_space(3))) * tr_ptr;
+            auto at = [&](int half) {
+                const int row = 32 * s + 8 * g + 4 * half + (t >> 2);
+                const int place = CF32 ? f * 2 + ((t >> 1) & 1) : (t & 3) * 2 + (f >> 1);
+                return row * 128 + 16 * swizzle<true, !CF32, 64>(place, row) + 8 * (CF32 ? t & 1 : f & 1);
+            };
+            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(L + at(0))), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(L + at(1)));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int row = CF32 ? f * 16 + t : (t >> 2) * 16 + f * 4 + (t & 3);
+            return *reinterpret_cast<const bf16x8*>(L + row * 128 + 16 * swizzle<false, !CF32, 64>(4 * s + g, row));
+        }
+    };
+    constexpr int ALWAYS = CHUNKS > 2 ? CHUNKS / 2 : 0;              // chunks that every S of this kernel has (two chunks: S >= 8)
+    const int inside = (int)(a.S / 32), most = (int)a.S - 8;         // chunks that no row ends in; where a row's last 16 bytes begin
+    std::conditional_t<ODD, AnyUnit, PlainUnit> p[CHUNKS];
+    u32x4_al now[CHUNKS];
+    auto ask = [&](int64_t r) {
+        const int64_t i = r * 16 + t < a.I ? r * 16 + t : a.I - 1;   // (a row past the end: any; it is not stored)
+        const char* const row = (const char*)a.P + i * a.ldp * 2;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int at = c * 32 + g * 8, from = c < ALWAYS || at < most ? at : most;      // (the last ones from the row's last 16 bytes)
+            p[c].load(row + from * 2);
+        }
+    };
+    const bool more = takes_more<OP>(a);
+    const int64_t first = (int64_t)blockIdx.x * TALL_WAVES + wave, stride = (int64_t)gridDim.x * TALL_WAVES;
+    if (first < rows_16) ask(first);
+    for (int64_t r = first; r < rows_16; r += stride) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            now[c] = p[c].value();
+            if (c >= ALWAYS && c >= inside) now[c] = moved_down<2>(now[c], c * 32 + g * 8 > most ? c * 32 + g * 8 - most : 0);
+        }
+        const int64_t row = r * 16 + t;
+        constexpr bool TB = OP == GRAD_X || !CF32;                   // the type of what a row takes besides
+        constexpr int N = CF32 ? 4 : 16, PARTS = CF32 ? 4 : 1;
+        RowPart<N, TB> further[PARTS];
+        auto ask_more = [&](int b) {
+#pragma unroll
+            for (int f = 0; f < PARTS; ++f) {
+                const int col = (int)j0 + b * 64 + (CF32 ? 16 * f + 4 * g : 16 * g);
+                if (more && row < a.I && col < a.J) load_more<OP>(a, row, col, further[f]);
+            }
+        };
+        ask_more(0);
+        if (r + stride < rows_16) ask(r + stride);
+        for (int b = 0; b < mine; ++b) {
+            floatx4 acc[4];
+#pragma unroll
+            for (int f = 0; f < 4; ++f) acc[f] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(b, f, c), __builtin_bit_cast(bf16x8, now[c]), acc[f], 0, 0, 0);
+            RowPart<N, TB> these[PARTS];
+#pragma unroll
+            for (int f = 0; f < PARTS; ++f) these[f] = further[f];
+            if (b + 1 < mine) ask_more(b + 1);
+#pragma unroll
+            for (int f = 0; f < PARTS; ++f) {
+                const int in = b * 64 + (CF32 ? 16 * f + 4 * g : 16 * g), col = (int)j0 + in;
+                if (row < a.I && col < a.J) {
+                    ColumnTerms<OP, N> terms;
+                    if constexpr (OP == FWD_BF16)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) terms.bias.w[e] = __float_as_uint(lds_bias[in + e]);
+                    float v[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[e] = acc[CF32 ? f : e >> 2][e & 3];
+                    finish<OP, N, TB>(a, row, col, v, terms, more, these[f]);
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ rows that are no whole units
+// An operand's rows copied to whole units of 16 bytes, zeros behind them: tiles of such rows go straight into LDS, where others come by way of registers
+// (8192 x 4096, K = 4096 211 us, with rows of 4097 549: for 2 x 33 MB more the first is had again).
+struct PackOperand {
+    const void* from;
+    int64_t ld, rows, length;           // elements
+    void* to;
+    int64_t units;                      // of a row
+};
+template <int ES> __global__ __launch_bounds__(256) void linear_pack_kernel(PackOperand a, PackOperand b) {
+    const uint32_t all = (uint32_t)(a.rows * a.units), both = all + (uint32_t)(b.rows * b.units);
+    for (uint32_t u0 = blockIdx.x * 1024 + threadIdx.x; u0 < both; u0 += gridDim.x * 1024) {
+        u32x4_al v[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {                        // four loads on their way
+            const uint32_t u = u0 + k * 256, in = u < all ? u : u - all;
+            if (u >= both) break;
+            const PackOperand& o = u < all ? a : b;
+            const uint32_t row = in / (uint32_t)o.units, at = in - row * (uint32_t)o.units;
+            v[k] = load_part<ES>((const char*)o.from + row * o.ld * ES, at * (16 / ES), o.length);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t u = u0 + k * 256;
+            if (u < both) reinterpret_cast<u32x4_al*>((u < all ? a : b).to)[u < all ? u : u - all] = v[k];
+        }
+    }
+}
+constexpr int64_t MOST_PACKED = (int64_t)3 << 30;       // units of both operands, which are counted in 32 bits
+
 // ------------------------------------------------------------------ host
 struct LinearPlan {
     int shape = 0;                      // of LINEAR_TILES
     int few = 0;                        // fragments of rows of linear_few_kernel (0: tiles)
+    bool tall = false;                  // linear_tall_kernel, whatever the alignment
+    size_t packed_p = 0, packed_q = 0;  // bytes of the operands' copies as whole units (0: none)
     int64_t steps = 0, per_split = 0;
     int32_t tiles_i = 0, tiles_j = 0, splits = 1, ld_part = 0;
     size_t bytes = 0;
@@ -789,32 +960,26 @@ constexpr int CUS = 256;
 // and for splits a second launch (3.5 us, with what the host takes for it) that reads the partial sums.  Against the best of all tiles and splits, on 90
 // products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 12 % at most, dw 2.6 % and 26 %.  Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096,
 // K = 4096: 256 x 256 211, 128 x 128 258; 512 x 256, K = 256: 64 x 128 8.0, 256 x 256 15.8; dw over 8192 rows, 256 x 256: 64 x 128 in 16 splits 14.6, unsplit 81.
-LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
-    LinearPlan p;
-    p.steps = std::max<int64_t>(1, cdiv(S, 128 / elem_size(op)));
-    const int64_t s_bytes = S * elem_size(op);
-    // Few rows: one launch, as long as the sums are not so long that the CUs without a workgroup would have halved the time.  Forward of bf16, J = 4096, us, this and
-    // tiles: 1 row, K = 2048 7.5 and 9.1, K = 4096 14.1 and 11.0; 32 rows, K = 2048 8.3 and 12.1; 64 rows, K = 1024 8.2 and 12.6, K = 2048 (J = 256) 11.3 and 11.1.
-    if (op != GRAD_W && I <= 64 && J >= 2 && s_bytes <= (I <= 32 ? 6144 : 3072)) {
-        p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
-        p.tiles_j = (int32_t)cdiv(J, 32);
-        return p;
-    }
+bool may_be_tall(int op, int64_t S) { return (op == FWD_BF16 || op == GRAD_X) && S >= 8 && (S <= 256 || (S <= 512 && S % 2 == 0)); }
+
+//   By way of registers (rows that are no whole units): 128 x 128 tiles, whose step then takes 2.1 us alone and 3.1 with another on the CU, and 9 us at least.
+double search_tiles(LinearPlan& p, int op, int64_t I, int32_t J, bool registers) {
     double best = 0.0;
     const double extra = op == GRAD_W ? 1.0 : 0.0;
-    for (int shape = 0; shape < 3; ++shape) {
+    for (int shape = registers ? 1 : 0; shape < (registers ? 2 : 3); ++shape) {
         const TileShape& t = LINEAR_TILES[shape];
         const double tiles = (double)cdiv(I, t.i) * (double)cdiv(J, t.j);
         for (int64_t splits = 1; splits <= p.steps && splits <= 512 && (splits == 1 || tiles * splits <= 16.0 * CUS); splits *= 2) {
             const int64_t per = cdiv(p.steps, splits), real = cdiv(p.steps, per);
             const double work = tiles * real;
             double rounds = 1.0;
-            int on = (int)std::min<double>(t.most, ceil(work / CUS));
+            const int on = (int)std::min<double>(t.most, ceil(work / CUS));
             if (work > (double)CUS * t.most) {
                 rounds = work / ((double)CUS * t.most);
                 rounds = rounds < 4.0 ? ceil(rounds) : rounds + 0.5;
             }
-            double us = 3.5 + std::max(rounds * (per * (double)t.step[on - 1] + t.besides * (0.5 + 0.5 * on)), work * per * (t.i + t.j) * 128.0 / 15e6);
+            const double step = registers ? 1.1 + on : (double)t.step[on - 1];
+            double us = (registers ? 7.0 : 3.5) + std::max(rounds * (per * step + t.besides * (0.5 + 0.5 * on)), work * per * (t.i + t.j) * 128.0 / 15e6);
             if (real > 1) us += 3.5 + ((double)I + extra) * J * 4.0 * real / 2.5e6 + 0.02 * real;
             if (best == 0.0 || us < best) {
                 best = us;
@@ -826,8 +991,46 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     }
     p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[p.shape].i);
     p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[p.shape].j);
+    return best;
+}
+
+LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
+    LinearPlan p;
+    p.steps = std::max<int64_t>(1, cdiv(S, 128 / elem_size(op)));
+    const int64_t s_bytes = S * elem_size(op);
+    // Few rows: one launch, as long as the sums are not so long that the CUs without a workgroup would have halved the time.  Forward of bf16, J = 4096, us, this and
+    // tiles: 1 row, K = 2048 7.5 and 9.1, K = 4096 14.1 and 11.0; 32 rows, K = 2048 8.3 and 12.1; 64 rows, K = 1024 8.2 and 12.6, K = 2048 (J = 256) 11.3 and 11.1.
+    if (op != GRAD_W && I <= 64 && J >= 2 && s_bytes <= (I <= 32 ? 6144 : 3072)) {
+        p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
+        p.tiles_j = (int32_t)cdiv(J, 32);
+        return p;
+    }
+    const int V = 16 / elem_size(op);
+    const bool odd_p = (p_columns(op) ? I : S) % V != 0, odd_q = (q_columns(op) ? J : S) % V != 0;      // rows that are no whole units
+    if (may_be_tall(op, S) && (odd_p || odd_q || (I >= 8192 && J <= 128 && s_bytes <= 512))) {
+        p.tall = true;
+        p.shape = 1;                    // (rows of more than 256 that begin at odd elements are left to tiles, unsplit)
+        p.per_split = p.steps;
+        p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[1].i);
+        p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[1].j);
+        return p;
+    }
+    if (!odd_p && !odd_q) {
+        search_tiles(p, op, I, J, false);
+    } else {
+        // as they are, or copied to whole units first: a launch, and 4.5 TB/s both ways
+        auto copy = [&](int64_t rows, int64_t length) { return (double)rows * (double)round_up(length, V) * elem_size(op); };
+        const double copy_p = odd_p ? p_columns(op) ? copy(S, I) : copy(I, S) : 0.0, copy_q = odd_q ? q_columns(op) ? copy(S, J) : copy(J, S) : 0.0;
+        LinearPlan whole = p;
+        const double packed = search_tiles(whole, op, I, J, false) + 3.5 + 2.0 * (copy_p + copy_q) / 4.5e6;
+        if (search_tiles(p, op, I, J, true) > packed && copy_p + copy_q < 16.0 * MOST_PACKED) {
+            p = whole;
+            p.packed_p = (size_t)round_up((int64_t)copy_p, 256);
+            p.packed_q = (size_t)round_up((int64_t)copy_q, 256);
+        }
+    }
     p.ld_part = (int32_t)round_up(J, 16);
-    if (p.splits > 1) p.bytes = (size_t)p.splits * (size_t)(I + (op == GRAD_W ? 1 : 0)) * p.ld_part * sizeof(float);
+    if (p.splits > 1) p.bytes = (size_t)round_up(p.splits * (I + (op == GRAD_W ? 1 : 0)) * p.ld_part * (int64_t)sizeof(float), 256);
     return p;
 }
 
@@ -837,36 +1040,100 @@ bool whole_units(const void* p, int64_t ld, int64_t n, int es) {
 }
 
 template <int OP> grp_status run_linear(const char* who, const char* name, LinearArgs a, double bytes, void* ws, size_t ws_bytes, hipStream_t st) {
+    constexpr int ES = elem_size(OP);
     const LinearPlan p = plan_of(OP, a.I, a.J, a.S);
     if ((int64_t)p.tiles_i * p.tiles_j * p.splits > MOST_TILES) return fail(GRP_EUNSUPPORTED, "%s: too large", who);
-    if (p.bytes && (!ws || ws_bytes < p.bytes)) return fail(GRP_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : (size_t)0, p.bytes);
-    if (p.bytes && (uintptr_t)ws % 16) return fail(GRP_EINVAL, "%s: workspace is not 16-byte aligned", who);
-    a.part = (float*)ws;
-    a.splits = p.splits;
-    a.ld_part = p.ld_part;
-    a.steps_per_split = p.per_split;
-    a.tiles_i = p.tiles_i;
-    a.tiles_j = p.tiles_j;
+    const size_t need = p.bytes + p.packed_p + p.packed_q;
+    if (need && (!ws || ws_bytes < need)) return fail(GRP_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : (size_t)0, need);
+    if (need && (uintptr_t)ws % 16) return fail(GRP_EINVAL, "%s: workspace is not 16-byte aligned", who);
+    const double flops = 2.0 * (double)a.I * a.J * a.S;
     if constexpr (OP != GRAD_W)
         if (p.few) {
-            ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
-            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_j, (unsigned)cdiv(a.I, 16 * p.few)), dim3(64 * FEW_WAVES), 0, st, a); };
+            ProfScope ps(name, st, flops, bytes);
+            auto go = [&](auto kernel) { a.tiles_j = p.tiles_j; hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_j, (unsigned)cdiv(a.I, 16 * p.few)), dim3(64 * FEW_WAVES), 0, st, a); };
             if (p.few == 1) go(linear_few_kernel<OP, 1>);
             else if (p.few == 2) go(linear_few_kernel<OP, 2>);
             else go(linear_few_kernel<OP, 4>);
             GRP_LAUNCH_CHECK();
             return GRP_OK;
         }
-    constexpr int ES = elem_size(OP);
-    const bool dma = whole_units(a.P, a.ldp, p_columns(OP) ? a.I : a.S, ES) && whole_units(a.Q, a.ldq, q_columns(OP) ? a.J : a.S, ES);
-    {
-        ProfScope ps(name, st, 2.0 * a.I * a.J * a.S, bytes);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles_i * p.tiles_j * p.splits)), dim3((unsigned)LINEAR_TILES[p.shape].threads), 0, st, a);
+    const int64_t length_p = p_columns(OP) ? a.I : a.S, length_q = q_columns(OP) ? a.J : a.S;
+    bool units_p = whole_units(a.P, a.ldp, length_p, ES), units_q = whole_units(a.Q, a.ldq, length_q, ES);
+    if constexpr (OP == FWD_BF16 || OP == GRAD_X)
+        if (const bool odd = (uintptr_t)a.P % 4 != 0 || a.ldp % 2 != 0; (p.tall || (may_be_tall(OP, a.S) && !(units_p && units_q))) && (a.S <= 256 || !odd)) {
+            ProfScope ps(name, st, flops, bytes);
+            const int64_t rows_16 = cdiv(a.I, 16), walks = cdiv(rows_16, TALL_WAVES);
+            const int chunks = a.S <= 64 ? 2 : a.S <= 128 ? 4 : a.S <= 256 ? 8 : 16, block_kb = chunks / 2 * 8;
+            const int columns = (int)cdiv(a.J, 64);
+            // as much of W as fits, but a workgroup for every CU
+            const int blocks = (int)std::min<int64_t>(std::min(columns, 128 / block_kb), std::max<int64_t>(1, columns * walks / CUS));
+            const int kb = blocks * block_kb <= 64 ? 64 : 128;
+            const int64_t groups = cdiv(columns, blocks), across = std::min<int64_t>(walks, round_up(cdiv((int64_t)CUS * (kb == 64 ? 2 : 1), groups), 8));
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)across, (unsigned)groups), dim3(64 * TALL_WAVES), 0, st, a, blocks, rows_16); };
+            auto by_type = [&](auto c, auto lds) {
+                constexpr int C = decltype(c)::value, KB = decltype(lds)::value;
+                auto by_row = [&](auto o) {
+                    if (a.c_bf16) go(linear_tall_kernel<OP, C, false, decltype(o)::value, KB>);
+                    else go(linear_tall_kernel<OP, C, true, decltype(o)::value, KB>);
+                };
+                if (!odd) by_row(std::false_type());
+                else if constexpr (C <= 8) by_row(std::true_type());
+            };
+            auto by_lds = [&](auto c) {
+                if (kb == 64) by_type(c, std::integral_constant<int, 64>());
+                else by_type(c, std::integral_constant<int, 128>());
+            };
+            if (chunks == 2) by_lds(std::integral_constant<int, 2>());
+            else if (chunks == 4) by_lds(std::integral_constant<int, 4>());
+            else if (chunks == 8) by_lds(std::integral_constant<int, 8>());
+            else by_lds(std::integral_constant<int, 16>());
+            GRP_LAUNCH_CHECK();
+            return GRP_OK;
+        }
+    a.end_p = (((p_columns(OP) ? a.S : a.I) - 1) * a.ldp + length_p) * ES;
+    a.end_q = (((q_columns(OP) ? a.S : a.J) - 1) * a.ldq + length_q) * ES;
+    if ((p.packed_p || p.packed_q) && (units_p || p.packed_p) && (units_q || p.packed_q)) {
+        char* at = (char*)ws + p.bytes;
+        PackOperand o[2] = {};
+        auto copy = [&](PackOperand& k, const void*& from, int64_t& ld, int64_t& end, bool columns, int64_t O, int64_t length, size_t size, bool& units) {
+            if (units) return;
+            k = PackOperand{from, ld, columns ? a.S : O, length, at, cdiv(length * ES, 16)};
+            from = at;
+            ld = k.units * 16 / ES;
+            end = k.rows * k.units * 16;
+            at += size;
+            units = true;
         };
-        if (p.shape == 0) { if (dma) go(linear_kernel<OP, 1, 2, 4, true>); else go(linear_kernel<OP, 1, 2, 4, false>); }
-        else if (p.shape == 1) { if (dma) go(linear_kernel<OP, 2, 2, 4, true>); else go(linear_kernel<OP, 2, 2, 4, false>); }
-        else { if (dma) go(linear_kernel<OP, 2, 4, 8, true>); else go(linear_kernel<OP, 2, 4, 8, false>); }
+        copy(o[0], a.P, a.ldp, a.end_p, p_columns(OP), a.I, length_p, p.packed_p, units_p);
+        copy(o[1], a.Q, a.ldq, a.end_q, q_columns(OP), a.J, length_q, p.packed_q, units_q);
+        const int64_t all = o[0].rows * o[0].units + o[1].rows * o[1].units;
+        if (all > 0) {
+            ProfScope ps("linear_pack", st, 0.0, 32.0 * all);
+            hipLaunchKernelGGL((linear_pack_kernel<ES>), dim3((unsigned)std::min<int64_t>(cdiv(all, 1024), 8192)), dim3(256), 0, st, o[0], o[1]);
+            GRP_LAUNCH_CHECK();
+        }
+    }
+    a.part = (float*)ws;
+    a.splits = p.splits;
+    a.ld_part = p.ld_part;
+    a.steps_per_split = p.per_split;
+    a.tiles_i = p.tiles_i;
+    a.tiles_j = p.tiles_j;
+    const bool dma = units_p && units_q;
+    if (!dma) {                         // by way of registers: those of 128 x 128 tiles suffice
+        a.tiles_i = (int32_t)cdiv(a.I, LINEAR_TILES[1].i);
+        a.tiles_j = (int32_t)cdiv(a.J, LINEAR_TILES[1].j);
+        if ((int64_t)a.tiles_i * a.tiles_j * p.splits > MOST_TILES) return fail(GRP_EUNSUPPORTED, "%s: too large", who);
+    }
+    {
+        ProfScope ps(name, st, flops, bytes);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_i * a.tiles_j * p.splits)), dim3((unsigned)LINEAR_TILES[dma ? p.shape : 1].threads), 0, st, a);
+        };
+        if (!dma) go(linear_kernel<OP, 2, 2, 4, false>);
+        else if (p.shape == 0) go(linear_kernel<OP, 1, 2, 4, true>);
+        else if (p.shape == 1) go(linear_kernel<OP, 2, 2, 4, true>);
+        else go(linear_kernel<OP, 2, 4, 8, true>);
         GRP_LAUNCH_CHECK();
     }
     if (p.splits > 1) {
@@ -890,10 +1157,11 @@ grp_status check_sizes(const char* who, int64_t m, int32_t n, int32_t k) {
 extern "C" size_t grp_linear_workspace_bytes(int32_t kind, int64_t m, int32_t n, int32_t k, int32_t dtype) {
     using namespace grp;
     if (m < 0 || n < 1 || k < 1) return 0;
-    if (kind == GRP_LINEAR_FORWARD) return plan_of(dtype == GRP_DTYPE_E4M3 ? FWD_E4M3 : FWD_BF16, m, n, k).bytes;
-    if (kind == GRP_LINEAR_DX) return plan_of(GRAD_X, m, k, n).bytes;
-    if (kind == GRP_LINEAR_DW) return plan_of(GRAD_W, k, n, m).bytes;
-    return 0;
+    if (kind != GRP_LINEAR_FORWARD && kind != GRP_LINEAR_DX && kind != GRP_LINEAR_DW) return 0;
+    const LinearPlan p = kind == GRP_LINEAR_FORWARD ? plan_of(dtype == GRP_DTYPE_E4M3 ? FWD_E4M3 : FWD_BF16, m, n, k)
+                         : kind == GRP_LINEAR_DX    ? plan_of(GRAD_X, m, k, n)
+                                                    : plan_of(GRAD_W, k, n, m);
+    return p.bytes + p.packed_p + p.packed_q;
 }
 
 extern "C" grp_status grp_linear(int64_t m, int32_t n, int32_t k, const void* a, int64_t lda, const void* w, int64_t ldw, int32_t dtype,
