@@ -676,30 +676,31 @@ template <int OP> __global__ __launch_bounds__(256) void linear_sum_kernel(Linea
 }
 
 // ------------------------------------------------------------------ few rows
-// Products of at most 64 rows are bound by reading W once.  A workgroup of sixteen wavefronts makes 16 MI rows and 32 columns; every wavefront takes blocks of
-// 128 bytes of s (all sixteen together consecutive ones) straight into registers, several in flight, and the sixteen sums are added in LDS: one
-// launch, however long the sums.  W by columns: a lane loads two columns of eight rows and turns them around with eight byte permutations.
-//   Lane (g, t) has D[t, 8 g + 2 e + f]: fragment f holds the columns 2 t + f.
-template <int OP> struct FewBlock {                    // a lane's part of 128 bytes of s
+// Products of at most 64 rows are bound by reading W once.  A workgroup of sixteen wavefronts makes 16 MI rows and 16 F columns; every wavefront takes blocks
+// of 128 bytes of s (all sixteen together consecutive ones) straight into registers, several in flight, and the sixteen sums are added in LDS: one
+// launch, however long the sums.  W by columns: 32 F bytes of 32 / F rows a load, turned around by way of LDS of the wavefront's own (with loads of
+// four bytes, which need no turning but byte permutations, a row times 4096 x 4096 took 14.1 us, now 11.7).  F = 1 where W has no more than 4096 columns, so that every
+// CU has a workgroup: the same 8.9 us (3.8 TB/s, of which some 2 us are the launch); 8192 columns, K = 4096 19.3 and, F = 2, 16.2.
+//   Lane (g, t) has D[t, 16 f + 4 g + e] in fragment f.
+template <int OP, int F> struct FewBlock {                  // a lane's part of 128 bytes of s
     static constexpr int ES = elem_size(OP), STEP = 128 / ES;
     static constexpr bool QC = q_columns(OP);
-    u32x4_al q[QC ? 1 : 4];                            // rows: fragment f's halves at 2 f, 2 f + 1
-    uint32_t c[QC ? 16 : 1];                           // columns: two of row 32 s + 8 g + k at 8 s + k
+    u32x4_al q[2 * F];  // rows: fragment f's halves at 2 f, 2 f + 1;  columns: row lane / 2F + 32 k / F of the block at k, columns 8 (lane % 2F) ..
 
-    // jc: the lane's columns (QC: two of J >= 2, from jc on) / rows of Q (jr[2]), all existing
-    __device__ __forceinline__ void load(const LinearArgs& a, int64_t s0, int g, int64_t jc, const int64_t (&jr)[2], bool whole) {
+    // jc, down: where a lane's columns begin and how far they are moved down (QC); jr: the lane's rows of Q, existing ones
+    __device__ __forceinline__ void load(const LinearArgs& a, int64_t s0, int lane, int64_t jc, const int64_t (&jr)[F], bool whole) {
         if constexpr (QC) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int64_t s = s0 + (k >> 3) * 32 + 8 * g + (k & 7);
-                c[k] = 0;
-                if (whole || s < a.S) c[k] = *reinterpret_cast<const u32_any*>((const uint16_t*)a.Q + s * a.ldq + jc);
+            for (int k = 0; k < 2 * F; ++k) {
+                const int64_t s = s0 + 32 / F * k + lane / (2 * F);
+                q[k] = u32x4_al{0, 0, 0, 0};
+                if (whole || s < a.S) q[k] = (u32x4_al)*reinterpret_cast<const u32x4_b*>((const uint16_t*)a.Q + s * a.ldq + jc);
             }
         } else {
 #pragma unroll
-            for (int f = 0; f < 2; ++f)
+            for (int f = 0; f < F; ++f)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) q[2 * f + h] = part_of(a.Q, a.ldq, jr[f], s0, a.S, 4 * h + g, whole);
+                for (int h = 0; h < 2; ++h) q[2 * f + h] = part_of(a.Q, a.ldq, jr[f], s0, a.S, 4 * h + (lane >> 4), whole);
         }
     }
     static __device__ __forceinline__ u32x4_al part_of(const void* base, int64_t ld, int64_t o, int64_t s0, int64_t S, int at, bool whole) {
@@ -708,46 +709,43 @@ template <int OP> struct FewBlock {                    // a lane's part of 128 b
         if (whole) return (u32x4_al)*reinterpret_cast<const u32x4_b*>(row + s * ES);
         return load_part<ES>(row, s, S);
     }
-    // fragment f's operand of half h (bf16 instructions)
-    __device__ __forceinline__ u32x4_al operand(int f, int h, int shift) const {
-        if constexpr (!QC) return q[2 * f + h];
-        u32x4_al v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = c[8 * h + 2 * k] >> shift, hi = c[8 * h + 2 * k + 1] >> shift;
-            v[k] = __builtin_amdgcn_perm(hi, lo, f ? 0x07060302u : 0x05040100u);
-        }
-        return v;
-    }
 };
 
 constexpr int FEW_WAVES = 16;
-template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a) {
-    typedef FewBlock<OP> Block;
+template <int OP, int MI, int F> __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearArgs a) {
+    typedef FewBlock<OP, F> Block;
     constexpr int STEP = Block::STEP, U = MI == 1 ? 4 : MI == 2 ? 2 : 1;
-    __shared__ float part[FEW_WAVES][16 * MI][36];
+    constexpr bool QC = Block::QC;
+    constexpr int PITCH = 16 * F + 4, OWN = QC && 16 * MI * PITCH < 512 * F ? 512 * F : 16 * MI * PITCH;       // a wavefront's LDS, in floats: a block to turn, then its sums
+    __shared__ __attribute__((aligned(16))) float part[FEW_WAVES * OWN];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, t = lane & 15;
-    // workgroups b and b + 8 run on one XCD: they share the lines of W's rows
-    const unsigned nb = (unsigned)a.tiles_j, b = blockIdx.x, pairs = nb / 16 * 16;
-    const unsigned col_block = b < pairs ? b / 16 * 16 + (b % 8) * 2 + (b / 8) % 2 : b;
-    const int64_t j0 = (int64_t)col_block * 32, i0 = (int64_t)blockIdx.y * 16 * MI;
-    const int64_t j = j0 + 2 * t, jc = j + 1 < a.J ? j : a.J - 2;
-    const int shift = j - jc == 1 ? 16 : 0;                                      // (the last column of an odd number; columns past the end: any)
-    const int64_t jr[2] = {j < a.J ? j : a.J - 1, j + 1 < a.J ? j + 1 : a.J - 1};
+    // workgroups b and b + 8 run on one XCD: those that share the lines of W's rows (of 64 columns) do
+    constexpr unsigned SHARE = 4 / F;
+    const unsigned nb = (unsigned)a.tiles_j, b = blockIdx.x, whole_groups = nb / (8 * SHARE) * (8 * SHARE);
+    const unsigned col_block = b < whole_groups ? b / (8 * SHARE) * (8 * SHARE) + (b % 8) * SHARE + (b / 8) % SHARE : b;
+    char* const turn = (char*)(part + wave * OWN);
+    const int64_t j0 = (int64_t)col_block * 16 * F, i0 = (int64_t)blockIdx.y * 16 * MI;
+    const int64_t j = j0 + 8 * (lane % (2 * F)), jc = j <= a.J - 8 ? j : a.J - 8;      // (the last columns from the row's last 16 bytes, moved down)
+    const bool edge = j0 + 16 * F > a.J;
+    int64_t jr[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) jr[f] = j0 + 16 * f + t < a.J ? j0 + 16 * f + t : a.J - 1;
     int64_t row[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) row[i] = i0 + 16 * i + t < a.I ? i0 + 16 * i + t : a.I - 1;
 
-    floatx4 acc[MI][2];
+    floatx4 acc[MI][F];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) acc[i][0] = acc[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int f = 0; f < F; ++f) acc[i][f] = floatx4{0.f, 0.f, 0.f, 0.f};
     auto take = [&](auto count, int64_t s0, bool whole) {
         constexpr int N = decltype(count)::value;
         Block q[N];
         u32x4_al p[N][MI][2];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            q[n].load(a, s0 + n * STEP, g, jc, jr, whole);
+            q[n].load(a, s0 + n * STEP, lane, jc, jr, whole);
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -755,9 +753,17 @@ template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void line
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) {
+            if constexpr (QC) {
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
+                for (int k = 0; k < 2 * F; ++k) {
+                    const u32x4_al v = edge ? moved_down<2>(q[n].q[k], j - jc) : q[n].q[k];
+                    *reinterpret_cast<u32x4_al*>(turn + 1024 * k + 16 * lane) = v;       // (rows of 32 F bytes)
+                }
+                __builtin_amdgcn_wave_barrier();                     // (a wavefront's accesses to LDS are made in order)
+            }
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
                 if constexpr (OP == FWD_E4M3) {
                     const intx8 w = __builtin_bit_cast(intx8, __builtin_shufflevector(q[n].q[2 * f], q[n].q[2 * f + 1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
@@ -766,12 +772,22 @@ template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void line
                 } else {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const u32x4_al w = q[n].operand(f, h, shift);
+                        u32x4_al w;
+                        if constexpr (QC) {
+                            typedef shortx4 __attribute__((address_space(3))) * tr_ptr;
+                            const char* at = turn + (32 * h + 8 * g + (t >> 2)) * (32 * F) + 32 * f + 8 * (t & 3);
+                            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 4 * 32 * F));
+                            w = __builtin_bit_cast(u32x4_al, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                        } else {
+                            w = q[n].q[2 * f + h];
+                        }
 #pragma unroll
                         for (int i = 0; i < MI; ++i) multiply<OP>(w, p[n][i][h], acc[i][f]);
                     }
                 }
             }
+            if constexpr (QC) __builtin_amdgcn_wave_barrier();
+        }
     };
     const int64_t full = a.S / STEP;
     int64_t k = (int64_t)wave * U;
@@ -781,15 +797,13 @@ template <int OP, int MI> __global__ __launch_bounds__(64 * FEW_WAVES) void line
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int f = 0; f < 2; ++f) part[wave][16 * i + t][8 * g + 2 * e + f] = acc[i][f][e];
+        for (int f = 0; f < F; ++f) *reinterpret_cast<floatx4*>(part + wave * OWN + (16 * i + t) * PITCH + 16 * f + 4 * g) = acc[i][f];
     __syncthreads();
-    const int r = threadIdx.x / 8, c4 = threadIdx.x % 8 * 4;
+    const int r = threadIdx.x / (4 * F), c4 = threadIdx.x % (4 * F) * 4;
     if (r >= 16 * MI || i0 + r >= a.I || j0 + c4 >= a.J) return;
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < FEW_WAVES; ++w) s += *reinterpret_cast<const floatx4*>(&part[w][r][c4]);
+    for (int w = 0; w < FEW_WAVES; ++w) s += *reinterpret_cast<const floatx4*>(part + w * OWN + r * PITCH + c4);
     float v[4] = {s[0], s[1], s[2], s[3]};
     for_more_type<OP>(a, [&](auto type) {
         RowPart<4, decltype(type)::value> terms;
@@ -942,7 +956,7 @@ constexpr int64_t MOST_PACKED = (int64_t)3 << 30;       // units of both operand
 // ------------------------------------------------------------------ host
 struct LinearPlan {
     int shape = 0;                      // of LINEAR_TILES
-    int few = 0;                        // fragments of rows of linear_few_kernel (0: tiles)
+    int few = 0, few_columns = 0;       // fragments of rows and columns of linear_few_kernel (0: tiles)
     bool tall = false;                  // linear_tall_kernel, whatever the alignment
     size_t packed_p = 0, packed_q = 0;  // bytes of the operands' copies as whole units (0: none)
     int64_t steps = 0, per_split = 0;
@@ -957,8 +971,8 @@ constexpr TileShape LINEAR_TILES[] = {{64, 128, 3, 128, {0.50f, 0.55f, 0.78f}, 1
 constexpr int CUS = 256;
 
 // The tile and the number of splits of the sums with the least time by a model of it: workgroups in rounds of what fits the CUs, 15 TB/s for the tiles' loads,
-// and for splits a second launch (3.5 us, with what the host takes for it) that reads the partial sums.  Against the best of all tiles and splits, on 90
-// products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 12 % at most, dw 2.6 % and 26 %.  Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096,
+// and for splits a second launch that reads the partial sums (1.5 us; two launches cost the host 9.5).  Against the best of all tiles and splits, on 90
+// products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 13 % at most, dw 2.0 % and 26 %.  Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096,
 // K = 4096: 256 x 256 211, 128 x 128 258; 512 x 256, K = 256: 64 x 128 8.0, 256 x 256 15.8; dw over 8192 rows, 256 x 256: 64 x 128 in 16 splits 14.6, unsplit 81.
 bool may_be_tall(int op, int64_t S) { return (op == FWD_BF16 || op == GRAD_X) && S >= 8 && (S <= 256 || (S <= 512 && S % 2 == 0)); }
 
@@ -980,7 +994,7 @@ double search_tiles(LinearPlan& p, int op, int64_t I, int32_t J, bool registers)
             }
             const double step = registers ? 1.1 + on : (double)t.step[on - 1];
             double us = (registers ? 7.0 : 3.5) + std::max(rounds * (per * step + t.besides * (0.5 + 0.5 * on)), work * per * (t.i + t.j) * 128.0 / 15e6);
-            if (real > 1) us += 3.5 + ((double)I + extra) * J * 4.0 * real / 2.5e6 + 0.02 * real;
+            if (real > 1) us = std::max(9.5, us + 1.5 + ((double)I + extra) * J * 4.0 * real / 3e6 + 0.02 * real);
             if (best == 0.0 || us < best) {
                 best = us;
                 p.shape = shape;
@@ -998,11 +1012,13 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     LinearPlan p;
     p.steps = std::max<int64_t>(1, cdiv(S, 128 / elem_size(op)));
     const int64_t s_bytes = S * elem_size(op);
-    // Few rows: one launch, as long as the sums are not so long that the CUs without a workgroup would have halved the time.  Forward of bf16, J = 4096, us, this and
-    // tiles: 1 row, K = 2048 7.5 and 9.1, K = 4096 14.1 and 11.0; 32 rows, K = 2048 8.3 and 12.1; 64 rows, K = 1024 8.2 and 12.6, K = 2048 (J = 256) 11.3 and 11.1.
-    if (op != GRAD_W && I <= 64 && J >= 2 && s_bytes <= (I <= 32 ? 6144 : 3072)) {
+    // Few rows: one launch, as long as the sums are not so long that tiles in splits, two launches, are faster.  Forward of bf16, J = 4096, us, this and tiles:
+    // 1 row, K = 4096 8.9 and 10.9, K = 8192 17.6 and 16.6; 32 rows, K = 2048 8.3 and 10.8, K = 4096 15.1 and 14.0; 64 rows, K = 1024 (J = 256) 7.0 and 9.3, K = 2048
+    // (J = 1024) 11.0 and 10.0.
+    if (op != GRAD_W && I <= 64 && J >= 8 && s_bytes <= (I <= 16 ? 8192 : I <= 32 ? 6144 : 3072)) {
         p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
-        p.tiles_j = (int32_t)cdiv(J, 32);
+        p.few_columns = J <= 16 * CUS ? 1 : 2;
+        p.tiles_j = (int32_t)cdiv(J, 16 * p.few_columns);
         return p;
     }
     const int V = 16 / elem_size(op);
@@ -1051,9 +1067,9 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
         if (p.few) {
             ProfScope ps(name, st, flops, bytes);
             auto go = [&](auto kernel) { a.tiles_j = p.tiles_j; hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_j, (unsigned)cdiv(a.I, 16 * p.few)), dim3(64 * FEW_WAVES), 0, st, a); };
-            if (p.few == 1) go(linear_few_kernel<OP, 1>);
-            else if (p.few == 2) go(linear_few_kernel<OP, 2>);
-            else go(linear_few_kernel<OP, 4>);
+            if (p.few == 1) { if (p.few_columns == 1) go(linear_few_kernel<OP, 1, 1>); else go(linear_few_kernel<OP, 1, 2>); }
+            else if (p.few == 2) { if (p.few_columns == 1) go(linear_few_kernel<OP, 2, 1>); else go(linear_few_kernel<OP, 2, 2>); }
+            else { if (p.few_columns == 1) go(linear_few_kernel<OP, 4, 1>); else go(linear_few_kernel<OP, 4, 2>); }
             GRP_LAUNCH_CHECK();
             return GRP_OK;
         }
