@@ -330,6 +330,19 @@ def test_linear(g, m, n, k, e8):
             assert torch.equal(c2.v, c.v)
 
 
+# sizes at which the other ways are taken: W kept in LDS (short sums, several groups of columns, rows at odd elements), copies as whole units, large tiles
+MORE_SHAPES = [(9000, 700, 60), (8200, 90, 300), (8193, 130, 257), (2000, 1030, 1021), (9000, 300, 515), (3000, 1001, 900), (6000, 2600, 136), (70, 520, 248), (12000, 61, 8),
+               (65, 9, 9)]
+
+
+@pytest.mark.parametrize("m,n,k", MORE_SHAPES)
+def test_linear_other_ways(g, m, n, k):
+    test_linear(g, m, n, k, False)
+    test_linear(g, m, n, k, True)
+    test_linear_dx(g, m, k, n)
+    test_linear_dw(g, m, n, k)
+
+
 @pytest.mark.parametrize("m,n,k", SHAPES)
 def test_linear_dx(g, m, n, k):
     for i, (pad, off, dt) in enumerate([(0, 0, FP32), (8, 0, BF16), (3, 1, BF16), (1, 0, FP32)]):
@@ -527,3 +540,38 @@ def test_equal_inputs_give_equal_bits_on_every_stream_and_in_graphs(g):
         check()
         block_pass(g, s)
         check()
+
+
+# ------------------------------------------------------------------------------------------------ large
+def test_offsets_past_32_bits(g):
+    """Rows that begin beyond 2^31 elements (and 2^32 bytes): the last ones, and those around the border."""
+    m, k, n = 140_001, 16_384, 16
+    r = gen(1)
+    a = torch.empty(m, k, device=DEV, dtype=BF16)
+    for i in range(0, m, 20_000):
+        a[i:i + 20_000] = torch.randn(min(20_000, m - i), k, generator=r, device=DEV)
+    rows = [0, 65_535, 65_536, 131_071, 131_072, 131_073, m - 1]
+    x = a[rows].double()
+    y = torch.empty_like(a)
+    g.grp_rmsnorm(m, k, a, k, g.DTYPE_BF16, None, 0, None, 1e-6, None, 0, y, k, g.DTYPE_BF16)
+    want = x / torch.sqrt(x.square().mean(1, keepdim=True) + 1e-6)
+    within(y[rows], want, want.abs() * (half_step(BF16) + 80 * U))
+    ws = torch.empty(g.grp_rmsnorm_backward_workspace_bytes(m, k), dtype=torch.uint8, device=DEV)
+    dw = torch.empty(k, device=DEV)
+    g.grp_rmsnorm_backward(m, k, a, k, g.DTYPE_BF16, a, k, g.DTYPE_BF16, None, 1e-6, None, 0, y, k, dw, ws)
+    dh, size, _, _ = norm_grad64(x, x, 1.0, 1e-6, 0.0)
+    within(y[rows], dh, dh.abs() * half_step(BF16) + size * 160 * U)
+    w = torch.randn(k, n, generator=r, device=DEV).to(BF16)
+    c = torch.empty(m, n, device=DEV)
+    g.grp_linear(m, n, k, a, k, w, n, g.DTYPE_BF16, None, None, None, g.ACT_NONE, None, 0, c, n, g.DTYPE_FP32, None, 0, workspace(g, 0, m, n, k, 1))
+    within(c[rows], x @ w.double(), (x.abs() @ w.double().abs()) * (k + 12) * 2 * U)
+    dz = torch.randn(m, n, generator=r, device=DEV).to(BF16)
+    dwt = torch.empty(k, n, device=DEV)
+    g.grp_linear_dw(m, n, k, a, k, dz, n, dwt, n, None, workspace(g, 2, m, n, k, 1))
+    for at in (slice(0, 32), slice(k - 32, k)):
+        p = a[:, at].double()
+        within(dwt[at], p.t() @ dz.double(), (p.abs().t() @ dz.double().abs()) * (m + 12) * 2 * U)
+    da = y
+    g.grp_linear_dx(m, n, k, dz, n, w, n, g.ACT_RELU, a, k, da, k, g.DTYPE_BF16, workspace(g, 1, m, n, k, 1))
+    lin = dz[rows].double() @ w.double().t()
+    within(da[rows], lin * (x > 0), (dz[rows].double().abs() @ w.double().abs().t()) * (n + 12) * 2 * U + lin.abs() * half_step(BF16) * 1.01)
