@@ -1038,23 +1038,36 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     const int V = 16 / elem_size(op);
     const int64_t length_p = p_columns(op) ? I : S, length_q = q_columns(op) ? J : S;      // of the operands' rows
     const bool odd_p = length_p % V != 0, odd_q = length_q % V != 0;                       // that are no whole units
-    if (may_be_tall(op, S) && (odd_p || odd_q || (I >= 8192 && J <= 128 && s_bytes <= 512))) {
+    auto take_tall = [&] {
         p.tall = true;
+        p.splits = 1;
         p.shape = 1;                    // (rows of more than 256 that begin at odd elements are left to tiles, unsplit)
         p.per_split = p.steps;
         p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[1].i);
         p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[1].j);
         return p;
-    }
+    };
     if (!odd_p && !odd_q) {
+        if (may_be_tall(op, S) && I >= 8192 && J <= 128 && s_bytes <= 512) return take_tall();
         search_tiles(p, op, I, J, false);
     } else {
-        // as they are, or copied to whole units first: a launch, and 4.5 TB/s both ways
+        // as they are, or copied to whole units first (a launch, and 4.5 TB/s both ways), or with W in LDS, which takes them at any alignment
         auto copy = [&](int64_t rows, int64_t length) { return (double)rows * (double)round_up(length, V) * elem_size(op); };
         const double copy_p = odd_p ? p_columns(op) ? copy(S, I) : copy(I, S) : 0.0, copy_q = odd_q ? q_columns(op) ? copy(S, J) : copy(J, S) : 0.0;
         LinearPlan whole = p;
-        const double packed = search_tiles(whole, op, I, J, false) + 3.5 + 2.0 * (copy_p + copy_q) / 4.5e6;
-        if (search_tiles(p, op, I, J, true) > packed && copy_p + copy_q < 16.0 * MOST_PACKED && length_p < (1 << 20) && length_q < (1 << 20)) {
+        double packed = search_tiles(whole, op, I, J, false), tiles = search_tiles(p, op, I, J, true);
+        if (may_be_tall(op, S)) {
+            // A wavefront's 16 rows and 64 columns take 0.3 us of a CU up to S = 128, 0.42 up to 256, then 0.35 + 0.0011 S; tiles are held to 4 TB/s for A and for C and
+            // one tensor like it.  us, this and copied tiles: 512 rows, 65 -> 1025 7.5 and 12; 3e5, 65 -> 65 48 and 57, 500 -> 129 189 and 293; 44 713, 376 -> 8175
+            // 1359 and 821.
+            const double memory = ((double)I * S * 2.0 + (double)I * J * 4.0) / 4e6;
+            const double tall = 6.5 + std::max(1.0, (double)cdiv(I, 16) * (double)cdiv(J, 64) / CUS) * (S <= 128 ? 0.3 : S <= 256 ? 0.42 : 0.35 + 0.0011 * S);
+            packed = std::max(packed, memory);
+            tiles = std::max(tiles, memory);
+            if (tall < std::min(tiles, packed + 3.5 + 2.0 * (copy_p + copy_q) / 4.5e6)) return take_tall();
+        }
+        packed += 3.5 + 2.0 * (copy_p + copy_q) / 4.5e6;
+        if (tiles > packed && copy_p + copy_q < 16.0 * MOST_PACKED && length_p < (1 << 20) && length_q < (1 << 20)) {
             p = whole;
             p.packed_p = (size_t)round_up((int64_t)copy_p, 256);
             p.packed_q = (size_t)round_up((int64_t)copy_q, 256);
@@ -1091,7 +1104,7 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
     const int64_t length_p = p_columns(OP) ? a.I : a.S, length_q = q_columns(OP) ? a.J : a.S;
     bool units_p = whole_units(a.P, a.ldp, length_p, ES), units_q = whole_units(a.Q, a.ldq, length_q, ES);
     if constexpr (OP == FWD_BF16 || OP == GRAD_X)
-        if (const bool odd = (uintptr_t)a.P % 4 != 0 || a.ldp % 2 != 0; (p.tall || (may_be_tall(OP, a.S) && !(units_p && units_q))) && (a.S <= 256 || !odd)) {
+        if (const bool odd = (uintptr_t)a.P % 4 != 0 || a.ldp % 2 != 0; (p.tall || (may_be_tall(OP, a.S) && !(units_p && units_q) && !p.packed_p && !p.packed_q)) && (a.S <= 256 || !odd)) {
             ProfScope ps(name, st, flops, bytes);
             const int64_t rows_16 = cdiv(a.I, 16), walks = cdiv(rows_16, TALL_WAVES);
             const int chunks = a.S <= 64 ? 2 : a.S <= 128 ? 4 : a.S <= 256 ? 8 : 16, block_kb = chunks / 2 * 8;
