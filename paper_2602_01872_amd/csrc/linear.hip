@@ -170,14 +170,17 @@ template <int N, bool BF16> __device__ __forceinline__ void store_row(void* p, i
 template <int OP, int N> struct ColumnTerms {
     RowPart<N, false> bias, ws;
     ColumnTerms() = default;
-    __device__ __forceinline__ ColumnTerms(const LinearArgs& a, int j) {
-        const int n = a.J - j;
-        if constexpr (is_forward(OP)) bias.load(a.bias + j, a.bias ? n : 0);
-        if constexpr (is_e4m3(OP)) {
-            ws.load(a.w_scale + j, a.w_scale ? n : 0);
-            if (!a.w_scale)
+    __device__ __forceinline__ ColumnTerms(const LinearArgs& a, int j, bool whole = false) {
+        const int n = whole ? N : a.J - j;
+        if constexpr (is_forward(OP)) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) ws.w[e] = 0x3F800000u;
+            for (int e = 0; e < N; ++e) bias.w[e] = 0;
+            if (a.bias) bias.load(a.bias + j, n);
+        }
+        if constexpr (is_e4m3(OP)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) ws.w[e] = 0x3F800000u;
+            if (a.w_scale) ws.load(a.w_scale + j, n);
         }
     }
 };
@@ -186,16 +189,21 @@ template <int OP, int N> struct ColumnTerms {
 template <int OP> __device__ __forceinline__ bool takes_more(const LinearArgs& a) {
     return is_forward(OP) ? a.r != nullptr : OP == GRAD_X && a.act != GRP_ACT_NONE;
 }
-template <int OP, int N, bool BF16> __device__ __forceinline__ void load_more(const LinearArgs& a, int64_t i, int j, RowPart<N, BF16>& t) {
+template <int OP, int N, bool BF16> __device__ __forceinline__ void load_more(const LinearArgs& a, int64_t i, int j, RowPart<N, BF16>& t, bool whole = false) {
     const int64_t at = is_forward(OP) ? i * a.ldr + j : i * a.ldz + j;
-    t.load((const char*)(is_forward(OP) ? a.r : a.z) + at * (BF16 ? 2 : 4), a.J - j);
+    t.load((const char*)(is_forward(OP) ? a.r : a.z) + at * (BF16 ? 2 : 4), whole ? N : a.J - j);
 }
 
-// D[i, j .. j + N - 1], all terms of the sums in v, to the outputs; more: takes_more, then t is load_more's.
-template <int OP, int N, bool BF16>
+// D[i, j .. j + N - 1], all terms of the sums in v, to the outputs; more: takes_more, then t is load_more's.  ACT: the activation where it is known (-1: not),
+// WHOLE: all N columns exist.
+template <int OP, int N, bool BF16, int ACT = -1, bool WHOLE = false>
 __device__ __forceinline__ void finish(const LinearArgs& a, int64_t i, int j, float (&v)[N], const ColumnTerms<OP, N>& col, bool more, const RowPart<N, BF16>& t) {
-    const int n = a.J - j;
+    const int n = WHOLE ? N : a.J - j;
     if (n <= 0) return;
+    auto with_act = [&](auto f) {
+        if constexpr (ACT < 0) for_act(a.act, f);
+        else if constexpr (ACT != GRP_ACT_NONE) f(std::integral_constant<int, ACT>());
+    };
     if constexpr (is_forward(OP)) {
         if constexpr (is_e4m3(OP)) {
             const float as = a.a_scale ? a.a_scale[i] : 1.f;
@@ -205,7 +213,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, int64_t i, int j, fl
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] += col.bias[e];
         if (a.z) store_row<N, true>((uint16_t*)a.z + i * a.ldz + j, n, v);
-        for_act(a.act, [&](auto act) {
+        with_act([&](auto act) {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] = act_of<decltype(act)::value>(v[e]);
         });
@@ -215,7 +223,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, int64_t i, int j, fl
         store_row<N, BF16>((char*)a.c + (i * a.ldc + j) * (BF16 ? 2 : 4), n, v);
     } else {
         if (more)
-            for_act(a.act, [&](auto act) {
+            with_act([&](auto act) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[e] *= slope_of<decltype(act)::value>(t[e]);
             });
@@ -610,20 +618,22 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
             for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(part + a.I * a.ld_part + col0 + 16 * g + 4 * f) = sums[f];
         return;
     }
-    for_more_type<OP>(a, [&](auto type) {
-        constexpr bool BF16 = decltype(type)::value;
-        constexpr int N = BF16 ? 8 : 4, UNITS = 32 / N;
+    auto rows_out = [&](auto type, auto activation, auto all_columns) {
+        constexpr bool BF16 = decltype(type)::value, WHOLE = decltype(all_columns)::value;
+        constexpr int N = BF16 ? 8 : 4, UNITS = 32 / N, ACT = decltype(activation)::value;
         constexpr int AHEAD = !BF16 ? 1 : OP == GRAD_X ? BATCHES : BATCHES < 2 ? BATCHES : 2;      // batches whose further terms are on their way: what registers allow
         const bool more = takes_more<OP>(a);
         const int col = col0 + lane % (64 / N) * N;
-        const ColumnTerms<OP, N> terms(a, col);
+        const bool here = col < a.J;
+        ColumnTerms<OP, N> terms;
+        if (here) terms = ColumnTerms<OP, N>(a, col, WHOLE);
         RowPart<N, BF16> further[AHEAD][UNITS];
         auto ask = [&](int b) {
-            if (more && col < a.J)
+            if (more && here)
 #pragma unroll
                 for (int u = 0; u < UNITS; ++u) {
                     const int64_t row = row0 + 32 * b + u * N + lane / (64 / N);
-                    if (row < a.I) load_more<OP>(a, row, col, further[b % AHEAD][u]);
+                    if (row < a.I) load_more<OP>(a, row, col, further[b % AHEAD][u], WHOLE);
                 }
         };
 #pragma unroll
@@ -637,10 +647,21 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
                 float v[N];
                 unit(std::integral_constant<int, N>(), u, v);
                 const int64_t row = row0 + 32 * b + u * N + lane / (64 / N);
-                if (row < a.I) finish<OP, N, BF16>(a, row, col, v, terms, more, further[b % AHEAD][u]);
+                if (here && row < a.I) finish<OP, N, BF16, ACT, WHOLE>(a, row, col, v, terms, more, further[b % AHEAD][u]);
             }
             if (b + AHEAD < BATCHES) ask(b + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // One run of code for each activation where a lane's columns all exist or none does: a small product spends a good part of its time on fetching code for
+    // the first time (512 x 256, K = 256 8.1 -> 7.1 us; 3e5 x 256 of K = 256 142 -> 134).
+    for_more_type<OP>(a, [&](auto type) {
+        if (col0 + 64 > a.J && a.J % (decltype(type)::value ? 8 : 4) != 0) {
+            rows_out(type, std::integral_constant<int, -1>(), std::false_type());
+        } else if (OP == GRAD_W || a.act == GRP_ACT_NONE) {
+            rows_out(type, std::integral_constant<int, GRP_ACT_NONE>(), std::true_type());
+        } else {
+            if constexpr (OP != GRAD_W) for_act(a.act, [&](auto act) { rows_out(type, act, std::true_type()); });
         }
     });
     if (OP == GRAD_W && make_sums && t == 0) {
