@@ -1050,7 +1050,7 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     // Few rows: one launch, as long as the sums are not so long that tiles in splits, two launches, are faster.  Forward of bf16, J = 4096, us, this and tiles:
     // 1 row, K = 4096 8.9 and 10.9, K = 8192 17.6 and 16.6; 32 rows, K = 2048 8.3 and 10.8, K = 4096 15.1 and 14.0; 64 rows, K = 1024 (J = 256) 7.0 and 9.3, K = 2048
     // (J = 1024) 11.0 and 10.0.
-    if (op != GRAD_W && I <= 64 && J >= 8 && s_bytes <= (I <= 16 ? 8192 : I <= 32 ? 6144 : 3072)) {
+    if (op != GRAD_W && I <= 64 && J >= 8 && s_bytes <= (I <= 16 ? 8 : I <= 32 ? 6 : 3) * 1024) {
         p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
         p.few_columns = J <= 16 * CUS ? 1 : 2;
         p.tiles_j = (int32_t)cdiv(J, 16 * p.few_columns);

@@ -6,6 +6,9 @@
 //
 // All arithmetic is fp32 (y is made from the sum x + r before that is rounded to h's type).  What bounds these kernels is memory: every input is
 // read once and every output written once, 16 bytes a lane, a row held in registers by the 8 .. 64 lanes of a wavefront or by a whole workgroup.
+//   Measured: 3e5 x 256 fp32 with the residual to bf16 183 us (5.9 TB/s), 8192 x 8192 bf16 with the residual to 8 bits 93 us (5.1 TB/s), 1e5 x 1004 bf16 to 8 bits
+// without a norm 53 us (5.7 TB/s), the gradient over 3e5 x 256 with the residual's 200 us (5.4 TB/s, 5 us of it the sum over 1024 workgroups' rows for the weight).
+// Rows of 257 instead of 256 bf16 146 and 105 us, of 8191 instead of 8192 119 and 104, of fp32 the same.
 #include "common.h"
 
 namespace grp {
@@ -234,18 +237,21 @@ __global__ __launch_bounds__(norm_threads(G)) void rmsnorm_kernel(NormArgs a) {
     }
 }
 
-// Lanes and units for rows of `units` units: the fewest lanes that hold a row in one unit each up to a wavefront, then up to `most_p` units, then
-// workgroups.  f(G, P) gets them as constants; false: too wide.
+// Lanes and units for rows of `units` units: the fewest lanes that hold a row in one unit each up to a wavefront, then two units a lane (the gradient, which
+// keeps five values of every column: half a wavefront and four), then workgroups.  f(G, P) gets them as constants; false: too wide.  us, this and another:
+//   3e5 x 256 bf16 norm 105, a quarter of the lanes with four units 117; 3e5 x 500 200 and 242; 1e5 x 1004 norm, 64 lanes with two 148, 32 with four 159, 256 with
+//   one 164; its gradient, 32 with four 157, 64 with two 183; 2e4 x 4096 norm, 256 with two 116, 1024 with one 138; 8192 x 8192, 1024 with one 93, 256 with four 104.
 template <int I> using int_c = std::integral_constant<int, I>;
-template <class F> bool for_row_shape(int64_t units, F f) {
+template <bool GRAD, class F> bool for_row_shape(int64_t units, F f) {
     if (units <= 8) f(int_c<8>(), int_c<1>());
     else if (units <= 16) f(int_c<16>(), int_c<1>());
     else if (units <= 32) f(int_c<32>(), int_c<1>());
     else if (units <= 64) f(int_c<64>(), int_c<1>());
-    else if (units <= 128) f(int_c<64>(), int_c<2>());
+    else if (units <= 128) f(int_c<GRAD ? 32 : 64>(), int_c<GRAD ? 4 : 2>());
     else if (units <= 256) f(int_c<256>(), int_c<1>());
     else if (units <= 512) f(int_c<256>(), int_c<2>());
-    else if (units <= 1024) f(int_c<256>(), int_c<4>());
+    else if (units <= 768) f(int_c<256>(), int_c<4>());
+    else if (units <= 1024) f(int_c<1024>(), int_c<1>());
     else if (units <= 2048) f(int_c<1024>(), int_c<2>());
     else if (units <= 4096) f(int_c<1024>(), int_c<4>());
     else if (units <= 8192) f(int_c<1024>(), int_c<8>());
@@ -261,7 +267,7 @@ template <typename XT, typename YT, bool NORM> grp_status launch_norm(const Norm
                            dim3(norm_threads(G)), 0, st, a);
     };
     if (a.width < V) go(int_c<1>(), int_c<8>(), int_c<1>());
-    else for_row_shape(cdiv(a.width, V), [&](auto G, auto P) { if constexpr (V * decltype(P)::value <= 32) go(int_c<V>(), G, P); });
+    else for_row_shape<false>(cdiv(a.width, V), [&](auto G, auto P) { if constexpr (V * decltype(P)::value <= 32) go(int_c<V>(), G, P); });
     GRP_LAUNCH_CHECK();
     return GRP_OK;
 }
@@ -415,7 +421,7 @@ GradPlan grad_plan(int64_t rows, int32_t width, bool wide /*both types bf16*/) {
     p.V = width < 8 ? 1 : wide ? 8 : 4;
     p.units = (int)cdiv(width, p.V);
     int rows_wg = 1;
-    for_row_shape(p.units, [&](auto G, auto) { rows_wg = norm_threads(G) / G; });
+    for_row_shape<true>(p.units, [&](auto G, auto) { rows_wg = norm_threads(G) / G; });
     // 1024 workgroups: four a CU, as many as run at once
     p.wgs = (int)std::min<int64_t>(1024, cdiv(rows, rows_wg));
     return p;
@@ -429,7 +435,7 @@ template <typename DT, typename HT> grp_status launch_norm_grad(NormGradArgs a, 
                            dim3(norm_threads(G)), 0, st, a);
     };
     if (p.V == 1) go(int_c<1>(), int_c<8>(), int_c<1>());
-    else for_row_shape(p.units, [&](auto G, auto P) { if constexpr (V * decltype(P)::value <= 32) go(int_c<V>(), G, P); });
+    else for_row_shape<true>(p.units, [&](auto G, auto P) { if constexpr (V * decltype(P)::value <= 32) go(int_c<V>(), G, P); });
     GRP_LAUNCH_CHECK();
     if (dweight) {
         hipLaunchKernelGGL(rmsnorm_grad_sum_kernel, dim3((unsigned)cdiv(a.width, 16)), dim3(1024), 0, st, a.part, p.wgs, a.ld_part, a.width, p.V, dweight);
