@@ -301,7 +301,6 @@ template <class Load, class Add> __device__ __forceinline__ void in_order(int c0
 // 16 and 8 bytes at any element boundary: global loads of these need no alignment beyond the element's
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t u32_any __attribute__((aligned(2)));
 // and at any byte, for 8-bit elements
 typedef uint32_t u32x4_b __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t u32x2_b __attribute__((ext_vector_type(2), aligned(1)));

@@ -8,8 +8,10 @@
 // result on normal deviates).  Beside the rounding of a bf16 result (rms 1.6e-3) that is nothing, and they run at twice the rate; for fp32 results
 // e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those.
 //
-// All are one kernel, D[i, j] = sum_s P(i, s) Q(s, j): an operand either has s contiguous ("rows": A, dZ, the 8-bit weights) or its output index
-// ("columns": W of the forward product, both operands of dw).  Products are accumulated in fp32 by the matrix unit.
+// All are D[i, j] = sum_s P(i, s) Q(s, j): an operand either has s contiguous ("rows": A, dZ, the 8-bit weights) or its output index ("columns": W of the
+// forward product, both operands of dw).  Products are accumulated in fp32 by the matrix unit.  Three kernels make them: tiles (linear_kernel, with
+// linear_sum_kernel where the sums are split), a few rows (linear_few_kernel), and many rows with short sums or rows at odd places (linear_tall_kernel); which one is
+// plan_of's choice.
 //
 // Tiles.  A workgroup of WI x WJ wavefronts makes 16 FI WI rows and 64 WJ columns; a step takes 128 bytes of s (64 bf16, 128 e4m3 numbers) of both operands
 // through LDS, two steps' tiles in turn, so that a step's loads have the whole step before to arrive.
@@ -17,6 +19,8 @@
 //   columns  LDS row s has the tile's output indices; ds_read_b64_tr_b16 turns four rows of 16 around into a lane's four consecutive s
 // Places are permuted by some bits of the row (swizzle) so that the 16 lanes of a group read different banks.
 //   The instruction's rows are D's columns: lane (g, t) holds D[i + t, j + 16 g + 4 f + e], e < 4, for the wavefront's fragments f < 4: 16 consecutive columns.
+//   Measured, 8192^3 with inputs that stay in the caches: forward 780 us (1410 TFLOP/s), dx 770 (1430), dw 800 (1370), 8 bits 370 (2990); the matrix unit is busy
+// 60 - 68 % of the cycles, a third of the rest goes to the loads (660 us without any), 256 x 256 tiles against 128 x 128: 790 and 1040 us (forward).
 #include "common.h"
 
 namespace grp {
@@ -470,7 +474,7 @@ template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__
     }
     const bool make_sums = OP == GRAD_W && ti == 0 && wi == 0 && a.db;
 
-    // byte of a lane's first operand; of the others see at_p, at_q
+    // byte of a lane's part of fragment f at half s of the step (columns: of its rows 4 half ..)
     auto at_p = [&](int f, int s, int half) {
         if constexpr (PC) {
             const int row = 32 * s + 8 * g + 4 * half + (t >> 2);
