@@ -4,6 +4,10 @@ the operators of residual blocks (``grappa.h``).
 A block is pre-norm:  h = x + r,  out = h + act(norm(h) W1 + b1) W2 + b2, where r is the block's own output of before (the norm adds it).
 Activations and the weights' copies are bf16, master weights, gradients and the optimizer's moments fp32 (one flat vector each, as
 ``grp_optimizer_step`` takes them).  ``serve`` runs the products in 8 bits, with weights quantized once.
+
+Parameters are set by writing into ``theta`` or its views ``params``: the next ``forward`` or ``serve`` makes the weights' copies anew.  That goes by torch's own
+count of writes, which a kernel of the user's own, a collective, a replayed graph and ``.data`` pass by: ``refresh()`` has to follow these.  A captured pass
+reads the copies at their places, as they are when it is replayed: after a write, ``refresh()`` comes before the replay.
 """
 from __future__ import annotations
 
@@ -15,6 +19,7 @@ from . import binding as g
 class ResidualBlocks:
     """``depth`` blocks of width ``dim`` with ``hidden`` units each, for at most ``rows`` rows at a time."""
 
+    @torch.inference_mode(False)        # (tensors of inference mode have no count of writes)
     def __init__(self, dim: int, hidden: int, depth: int, rows: int, act: int = g.ACT_GELU, eps: float = 1e-6, seed: int = 0, device="cuda"):
         if dim < 1 or hidden < 1 or depth < 1 or rows < 1:
             raise ValueError("dim, hidden, depth and rows must be positive")
@@ -22,13 +27,13 @@ class ResidualBlocks:
         shapes = [(dim,), (dim, hidden), (hidden,), (hidden, dim), (dim,)]            # norm, W1, b1, W2, b2
         sizes = [torch.Size(s).numel() for s in shapes]
         total = depth * sum(sizes)
-        self.theta = torch.zeros(total, device=device)
+        self._theta = torch.zeros(total, device=device)
         self.grad, self.m, self.v = (torch.zeros_like(self.theta) for _ in range(3))
         self.steps = 0
 
         def views(flat):
             parts = [p.view(s) for p, s in zip(flat.split(sizes * depth), shapes * depth)]
-            return [parts[5 * i:5 * i + 5] for i in range(depth)]
+            return [tuple(parts[5 * i:5 * i + 5]) for i in range(depth)]
 
         self.params, self.grads = views(self.theta), views(self.grad)
         gen = torch.Generator(device=device)
@@ -39,7 +44,7 @@ class ResidualBlocks:
             p[3].copy_(torch.randn(hidden, dim, generator=gen, device=device) * hidden ** -0.5 / depth)
         bf = dict(device=device, dtype=torch.bfloat16)
         self.w1, self.w2 = [torch.empty(dim, hidden, **bf) for _ in range(depth)], [torch.empty(hidden, dim, **bf) for _ in range(depth)]
-        self._served = None
+        self._served, self._quantized = None, None
         self._round_weights()
         # kept by forward for backward, per block: h, norm(h), the pre-activation and the activation; what a block adds to h
         self.h, self.y, self.out = ([torch.empty(rows, dim, **bf) for _ in range(depth)] for _ in range(3))
@@ -49,11 +54,26 @@ class ResidualBlocks:
         self.gradients = g.grp_gradients_create([self.grad])
         self.workspace = torch.empty(0, dtype=torch.uint8, device=device)
 
+    @property
+    def theta(self) -> torch.Tensor:
+        """All parameters, fp32; to be written into (``theta.copy_(saved)``), not replaced."""
+        return self._theta
+
+    def refresh(self):
+        """Makes the weights' copies anew: to be called after ``theta`` was written by what torch does not see."""
+        self._round_weights()
+        if self._served is not None:
+            self._weights8()
+
+    def _seen(self):
+        """The writes of ``theta`` that copies made now have seen: none where a graph is captured, which makes them at its replays."""
+        return None if self.theta.is_cuda and torch.cuda.is_current_stream_capturing() else self.theta._version
+
     def _round_weights(self):
         for i, p in enumerate(self.params):
             self.w1[i].copy_(p[1])
             self.w2[i].copy_(p[3])
-        self._served = None
+        self._rounded, self._quantized = self._seen(), None
 
     def _room(self, nbytes: int):
         if self.workspace.numel() < nbytes:
@@ -72,6 +92,8 @@ class ResidualBlocks:
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """``x``: bf16 [m x dim]; the result is kept until the next call."""
         m, d, f = self._check(x), self.dim, self.hidden
+        if self._rounded != self.theta._version:
+            self._round_weights()
         for i, p in enumerate(self.params):
             # the first block's input has nothing added; the others add what the block before made to its h
             src, add = (x, None) if i == 0 else (self.out[i - 1], self.h[i - 1])
@@ -104,14 +126,19 @@ class ResidualBlocks:
         self._round_weights()
         return self.norm
 
-    def _quantized(self):
+    def _weights8(self):
+        """The weights in 8 bits, [K x N] as rows of their transpose; made where theta was written, always in the same place."""
         if self._served is None:
-            def rows8(w):                                   # [K x N] -> rows of W^T in 8 bits
-                t = w.t().contiguous()
-                q, s = torch.empty(t.shape, dtype=torch.float8_e4m3fn, device=t.device), torch.empty(t.shape[0], device=t.device)
-                g.grp_quantize_rows(t.shape[0], t.shape[1], t, t.shape[1], g.DTYPE_FP32, q, t.shape[1], s)
-                return q, s
-            self._served = [(rows8(p[1]), rows8(p[3])) for p in self.params]
+            def room(w):
+                return torch.empty(w.shape[1], w.shape[0], dtype=torch.float8_e4m3fn, device=w.device), torch.empty(w.shape[1], device=w.device)
+            with torch.inference_mode(False):
+                self._served = [(room(p[1]), room(p[3])) for p in self.params]
+        if self._quantized != self.theta._version:
+            for p, pair in zip(self.params, self._served):
+                for w, (q, s) in zip((p[1], p[3]), pair):
+                    t = w.t().contiguous()
+                    g.grp_quantize_rows(t.shape[0], t.shape[1], t, t.shape[1], g.DTYPE_FP32, q, t.shape[1], s)
+            self._quantized = self._seen()
         return self._served
 
     def serve(self, x: torch.Tensor) -> torch.Tensor:
@@ -122,7 +149,7 @@ class ResidualBlocks:
         a8, s2 = torch.empty(m, f, dtype=torch.float8_e4m3fn, device=dev), torch.empty(m, device=dev)
         a, out = torch.empty(m, f, dtype=torch.bfloat16, device=dev), x
         ws = self._room(max(g.grp_linear_workspace_bytes(g.LINEAR_FORWARD, m, n, k, g.DTYPE_E4M3) for n, k in ((f, d), (d, f))))
-        for (p, ((w1, w1s), (w2, w2s))) in zip(self.params, self._quantized()):
+        for (p, ((w1, w1s), (w2, w2s))) in zip(self.params, self._weights8()):
             nxt = torch.empty_like(x)
             g.grp_rmsnorm(m, d, out, d, g.DTYPE_BF16, None, 0, p[0], self.eps, None, 0, y8, d, g.DTYPE_E4M3, s1)
             g.grp_linear(m, f, d, y8, d, w1, d, g.DTYPE_E4M3, s1, w1s, p[2], self.act, None, 0, a, f, g.DTYPE_BF16, None, 0, ws)

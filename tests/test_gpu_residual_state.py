@@ -1,0 +1,83 @@
+"""What the head of residual blocks keeps, on the GPU: parameters that are set, rows, streams and captured passes."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_2602_01872_amd as lib
+    lib.load()
+    return lib
+
+
+def rows_of(n, dim, seed=5):
+    r = torch.Generator(device=DEV)
+    r.manual_seed(seed)
+    return torch.randn(n, dim, generator=r, device=DEV).to(torch.bfloat16)
+
+
+def results(b, x):
+    return b.forward(x).clone(), b.serve(x).clone()
+
+
+def same(got, want):
+    return all(torch.equal(s, t) for s, t in zip(got, want))
+
+
+def test_loaded_parameters_are_the_ones_that_are_used(g):
+    a, b = g.ResidualBlocks(64, 128, 2, 50, seed=1), g.ResidualBlocks(64, 128, 2, 50, seed=2)
+    x = rows_of(50, 64)
+    want = results(a, x)
+    assert not same(results(b, x), want)
+    b.theta.copy_(a.theta)
+    assert same(results(b, x), want)
+    b.theta.mul_(0.5)
+    assert not same(results(b, x), want)
+    b.theta.data.copy_(a.theta)
+    b.refresh()
+    assert same(results(b, x), want)
+    opt = g.optimizer_desc(g.OPT_SGD, lr=0.1)
+    b.forward(x)
+    b.backward(x)
+    b.step(opt, 1.0)
+    a.theta.copy_(b.theta)
+    assert same(results(a, x), results(b, x)) and not same(results(a, x), want)
+
+
+def test_captured_passes_follow_parameters(g):
+    """A replay reads the copies as they are then; a pass that is captured with copies out of date makes them at every replay, and marks none as made."""
+    a, b = g.ResidualBlocks(64, 128, 2, 50, seed=1), g.ResidualBlocks(64, 128, 2, 50, seed=2)
+    x = rows_of(50, 64)
+    want, first = results(a, x), results(b, x)
+
+    def captured(blocks):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = blocks.forward(x).clone(), blocks.serve(x)
+        return graph, out
+
+    def replayed(graph, out):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        return out
+
+    graph, out = captured(b)
+    assert same(replayed(graph, out), first)
+    b.theta.copy_(a.theta)
+    b.refresh()
+    for _ in range(3):
+        assert same(replayed(graph, out), want)
+        assert same(results(b, x), want)
+    late = g.ResidualBlocks(64, 128, 2, 50, seed=3)
+    late.theta.copy_(a.theta)
+    graph, out = captured(late)
+    assert same(results(late, x), want)              # before any replay
+    late.theta.copy_(b.theta * 0.5)
+    want = results(late, x)
+    for _ in range(3):
+        assert same(replayed(graph, out), want)
