@@ -8,6 +8,11 @@ Activations and the weights' copies are bf16, master weights, gradients and the 
 Parameters are set by writing into ``theta`` or its views ``params``: the next ``forward`` or ``serve`` makes the weights' copies anew.  That goes by torch's own
 count of writes, which a kernel of the user's own, a collective, a replayed graph and ``.data`` pass by: ``refresh()`` has to follow these.  A captured pass
 reads the copies at their places, as they are when it is replayed: after a write, ``refresh()`` comes before the replay.
+
+Streams: ``forward``, ``backward`` and ``step`` work on what the object keeps, so they are ordered one after another by the caller, as calls on one stream are.
+``serve`` keeps nothing of a call: several may run side by side on streams of their own, after the writes of ``theta`` (the constructor's, ``step``'s) and
+before the next; the 8-bit weights that the first one makes are waited for by the others.  A capture does not wait: a ``serve`` goes before it.  The object
+outlives the work on all of them.
 """
 from __future__ import annotations
 
@@ -44,7 +49,7 @@ class ResidualBlocks:
             p[3].copy_(torch.randn(hidden, dim, generator=gen, device=device) * hidden ** -0.5 / depth)
         bf = dict(device=device, dtype=torch.bfloat16)
         self.w1, self.w2 = [torch.empty(dim, hidden, **bf) for _ in range(depth)], [torch.empty(hidden, dim, **bf) for _ in range(depth)]
-        self._served, self._quantized = None, None
+        self._served, self._quantized, self._made = None, None, None
         self._round_weights()
         # kept by forward for backward, per block: h, norm(h), the pre-activation and the activation; what a block adds to h
         self.h, self.y, self.out = ([torch.empty(rows, dim, **bf) for _ in range(depth)] for _ in range(3))
@@ -52,7 +57,6 @@ class ResidualBlocks:
         self.dh, self.dy, self.dz = torch.empty(rows, dim, **bf), torch.empty(rows, dim, **bf), torch.empty(rows, hidden, **bf)
         self.norm = torch.zeros(1, device=device)
         self.gradients = g.grp_gradients_create([self.grad])
-        self.workspace = torch.empty(0, dtype=torch.uint8, device=device)
 
     @property
     def theta(self) -> torch.Tensor:
@@ -76,9 +80,8 @@ class ResidualBlocks:
         self._rounded, self._quantized = self._seen(), None
 
     def _room(self, nbytes: int):
-        if self.workspace.numel() < nbytes:
-            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.theta.device)
-        return self.workspace
+        """A workspace for the calls that follow on the current stream (kept by a graph that is captured as long as it lives)."""
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.theta.device)
 
     def _linear(self, m, n, k, a, w, bias, act, r, c, z):
         ws = self._room(g.grp_linear_workspace_bytes(g.LINEAR_FORWARD, m, n, k, g.DTYPE_BF16))
@@ -127,7 +130,7 @@ class ResidualBlocks:
         return self.norm
 
     def _weights8(self):
-        """The weights in 8 bits, [K x N] as rows of their transpose; made where theta was written, always in the same place."""
+        """The weights in 8 bits, [K x N] as rows of their transpose; made where theta was written, always in the same place, and waited for by other streams."""
         if self._served is None:
             def room(w):
                 return torch.empty(w.shape[1], w.shape[0], dtype=torch.float8_e4m3fn, device=w.device), torch.empty(w.shape[1], device=w.device)
@@ -139,6 +142,10 @@ class ResidualBlocks:
                     t = w.t().contiguous()
                     g.grp_quantize_rows(t.shape[0], t.shape[1], t, t.shape[1], g.DTYPE_FP32, q, t.shape[1], s)
             self._quantized = self._seen()
+            if self._quantized is not None and self.theta.is_cuda:
+                self._made = g._stream(None), torch.cuda.current_stream().record_event()
+        elif self._made is not None and self._made[0] != g._stream(None) and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().wait_event(self._made[1])
         return self._served
 
     def serve(self, x: torch.Tensor) -> torch.Tensor:

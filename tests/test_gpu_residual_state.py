@@ -81,3 +81,49 @@ def test_captured_passes_follow_parameters(g):
     want = results(late, x)
     for _ in range(3):
         assert same(replayed(graph, out), want)
+
+
+def test_serves_side_by_side(g):
+    """Each stream's results are what one stream gives, from the first call on, which makes the 8-bit weights; sizes whose products are split."""
+    dim, hidden, rows = 512, 2048, 200
+    assert g.grp_linear_workspace_bytes(g.LINEAR_FORWARD, rows, dim, hidden, g.DTYPE_E4M3) > 0
+    b, other = (g.ResidualBlocks(dim, hidden, 2, rows, seed=1) for _ in range(2))
+    xs = [rows_of(rows, dim, seed) for seed in range(4)]
+    want = [other.serve(x).clone() for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out = []
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                out.append(b.serve(x))
+        torch.cuda.synchronize()
+        assert same(out, want)
+        b.theta.mul_(1.0)                            # the copies are made again
+        torch.cuda.synchronize()
+
+
+def test_a_captured_pass_keeps_its_workspace(g):
+    """Replays between passes of other sizes, which ask for more room."""
+    dim, hidden, rows = 256, 512, 3000
+    b = g.ResidualBlocks(dim, hidden, 2, rows, seed=1)
+    x, dout, big = rows_of(300, dim), rows_of(300, dim, 6), rows_of(rows, dim, 7)
+
+    def step(v, d):
+        out = b.forward(v).clone()
+        dx = b.backward(d).clone()
+        return [out, dx, b.serve(v), b.grad.clone()]
+
+    want = step(x, dout)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, dout)
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got, want)
+        step(big, big)
+        junk = torch.full((64 << 20,), 255, dtype=torch.uint8, device=DEV)     # takes what was given back
+        del junk

@@ -178,3 +178,18 @@ def test_the_weights_copies_stay_where_they_are(ops, monkeypatch):
         places.append(seen)
         b.theta.mul_(2)
     assert places[0] == places[1]
+
+
+def test_no_workspace_is_kept(ops):
+    """Calls that run side by side on two streams, a captured pass and a later larger one: each writes its own partial sums."""
+    b = make()
+    x = rows_of(6)
+    b.forward(x)
+    b.backward(x)
+    b.serve(x[:1].contiguous())
+    b.serve(x)
+    own = {t.untyped_storage().data_ptr() for t in vars(b).values() if torch.is_tensor(t)}
+    assert len(ops.workspaces) > 12
+    for ws in ops.workspaces:
+        assert ws.numel() >= 64 and ws.untyped_storage().data_ptr() not in own
+    assert all(ws.untyped_storage().data_ptr() != other.untyped_storage().data_ptr() for ws in ops.workspaces[-4:] for other in ops.workspaces[:-8])
