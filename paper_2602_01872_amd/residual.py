@@ -51,6 +51,7 @@ class ResidualBlocks:
         self.w1, self.w2 = [torch.empty(dim, hidden, **bf) for _ in range(depth)], [torch.empty(hidden, dim, **bf) for _ in range(depth)]
         self._served, self._quantized, self._made = None, None, None
         self._round_weights()
+        self._kept = None                   # rows of the last forward pass
         # kept by forward for backward, per block: h, norm(h), the pre-activation and the activation; what a block adds to h
         self.h, self.y, self.out = ([torch.empty(rows, dim, **bf) for _ in range(depth)] for _ in range(3))
         self.z, self.a = ([torch.empty(rows, hidden, **bf) for _ in range(depth)] for _ in range(2))
@@ -95,6 +96,7 @@ class ResidualBlocks:
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """``x``: bf16 [m x dim]; the result is kept until the next call."""
         m, d, f = self._check(x), self.dim, self.hidden
+        self._kept = None
         if self._rounded != self.theta._version:
             self._round_weights()
         for i, p in enumerate(self.params):
@@ -104,11 +106,14 @@ class ResidualBlocks:
             self._linear(m, f, d, self.y[i], self.w1[i], p[2], self.act, None, self.a[i], self.z[i])
             last = i == self.depth - 1
             self._linear(m, d, f, self.a[i], self.w2[i], p[4], g.ACT_NONE, self.h[i] if last else None, self.out[i], None)
+        self._kept = m
         return self.out[-1][:m]
 
     def backward(self, dout: torch.Tensor) -> torch.Tensor:
-        """Gradients of the parameters (``grad``) and of ``x`` from the result's, for the rows of the last ``forward``."""
+        """Gradients of the parameters (``grad``) and of ``x`` from the result's, for the rows of the last ``forward``, as many as it had."""
         m, d, f = self._check(dout), self.dim, self.hidden
+        if m != self._kept:
+            raise ValueError(f"the gradient has {m} rows, the last forward pass {'was not made' if self._kept is None else f'had {self._kept}'}")
         self.dh[:m].copy_(dout)
         for i in reversed(range(self.depth)):
             p, q = self.params[i], self.grads[i]

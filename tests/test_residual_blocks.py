@@ -193,3 +193,22 @@ def test_no_workspace_is_kept(ops):
     for ws in ops.workspaces:
         assert ws.numel() >= 64 and ws.untyped_storage().data_ptr() not in own
     assert all(ws.untyped_storage().data_ptr() != other.untyped_storage().data_ptr() for ws in ops.workspaces[-4:] for other in ops.workspaces[:-8])
+
+
+def test_backward_takes_the_rows_of_the_last_forward(ops):
+    b = make(rows=10)
+    with pytest.raises(ValueError):          # nothing is kept yet
+        b.backward(rows_of(4))
+    b.forward(rows_of(10))
+    b.forward(rows_of(4))
+    for n in (10, 5, 3, 0):
+        with pytest.raises(ValueError):
+            b.backward(rows_of(n))
+    b.serve(rows_of(10))                     # keeps nothing
+    b.backward(rows_of(4))
+    b.backward(rows_of(4))                   # the kept rows are still there
+    with pytest.raises(ValueError):          # a refused call leaves them
+        b.forward(rows_of(11))
+    b.backward(rows_of(4))
+    b.forward(rows_of(0))
+    b.backward(rows_of(0))
