@@ -620,10 +620,12 @@ def grp_gradients_create(grads, outs=None) -> Gradients:
     """``grads``: contiguous float32 or bfloat16 device tensors; ``outs``: tensors of the same shapes and types for the clipped gradient (None: in
     place)."""
     kinds = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} tensors and {len(outs)} outputs")
     for i, t in enumerate(grads):
         o = t if outs is None else outs[i]
-        if t.dtype not in kinds or not t.is_contiguous() or not o.is_contiguous() or o.dtype != t.dtype or o.numel() != t.numel():
-            raise ValueError(f"tensor {i}: contiguous float32 or bfloat16 is needed, and an output of the same type and size")
+        if t.dtype not in kinds or not t.is_contiguous() or not o.is_contiguous() or o.dtype != t.dtype or o.numel() != t.numel() or not (t.is_cuda and o.is_cuda):
+            raise ValueError(f"tensor {i}: contiguous float32 or bfloat16 on the GPU is needed, and an output of the same type and size")
     n = len(grads)
     ptrs = lambda ts: (C.c_void_p * n)(*[_ptr(t) for t in ts])
     out = C.c_void_p()

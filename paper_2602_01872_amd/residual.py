@@ -89,8 +89,8 @@ class ResidualBlocks:
         g.grp_linear(m, n, k, a, k, w, n, g.DTYPE_BF16, None, None, bias, act, r, n, c, n, g.DTYPE_BF16, z, n, ws)
 
     def _check(self, x):
-        if x.dtype != torch.bfloat16 or x.dim() != 2 or x.shape[1] != self.dim or x.shape[0] > self.rows or not x.is_contiguous():
-            raise ValueError(f"rows of {self.dim} bfloat16 numbers are needed, at most {self.rows}, contiguous")
+        if x.dtype != torch.bfloat16 or x.dim() != 2 or x.shape[1] != self.dim or x.shape[0] > self.rows or not x.is_contiguous() or x.device != self.theta.device:
+            raise ValueError(f"rows of {self.dim} bfloat16 numbers are needed, at most {self.rows}, contiguous, on {self.theta.device}")
         return x.shape[0]
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:

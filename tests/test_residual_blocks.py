@@ -212,3 +212,22 @@ def test_backward_takes_the_rows_of_the_last_forward(ops):
     b.backward(rows_of(4))
     b.forward(rows_of(0))
     b.backward(rows_of(0))
+
+
+def test_tensors_of_another_device_are_refused(ops):
+    """A kernel that is handed host memory faults."""
+    b = make()
+    elsewhere = torch.empty(4, 16, dtype=BF16, device="meta")
+    for call in (b.forward, b.backward, b.serve):
+        with pytest.raises(ValueError):
+            call(elsewhere)
+
+
+def test_gradients_on_the_host_are_refused():
+    host = torch.zeros(8)
+    with pytest.raises(ValueError):
+        binding.grp_gradients_create([host])
+    with pytest.raises(ValueError):
+        binding.grp_gradients_create([torch.empty(8, device="meta")], [host])
+    with pytest.raises(ValueError):          # an output for every tensor
+        binding.grp_gradients_create([torch.empty(8, device="meta")], [])
