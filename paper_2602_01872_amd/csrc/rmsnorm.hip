@@ -122,6 +122,11 @@ struct NormArgs {
 
 constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
 
+}  // namespace
+// Rows of G lanes each that one launch takes: a launch holds fewer than 2^32 work-items.
+int64_t norm_rows_of_launch(int G) { return (int64_t)((1u << 31) / norm_threads(G)) * (norm_threads(G) / G); }
+namespace {
+
 // G lanes a row, P units a lane.
 template <typename XT, typename YT, bool NORM, int V, int G, int P>
 __global__ __launch_bounds__(norm_threads(G)) void rmsnorm_kernel(NormArgs a) {
@@ -263,8 +268,18 @@ template <typename XT, typename YT, bool NORM> grp_status launch_norm(const Norm
     constexpr int V = 16 / sizeof(XT);
     auto go = [&](auto v, auto G, auto P) {
         constexpr int rows = norm_threads(G) / G;
-        hipLaunchKernelGGL((rmsnorm_kernel<XT, YT, NORM, decltype(v)::value, decltype(G)::value, decltype(P)::value>), dim3((unsigned)cdiv(a.rows, rows)),
-                           dim3(norm_threads(G)), 0, st, a);
+        const int64_t most = norm_rows_of_launch(G);
+        for (int64_t at = 0; at < a.rows; at += most) {
+            NormArgs b = a;
+            b.rows = std::min(most, a.rows - at);
+            b.x = (const XT*)a.x + at * a.ldx;
+            if (a.r) b.r = (const XT*)a.r + at * a.ldr;
+            if (a.h) b.h = (XT*)a.h + at * a.ldh;
+            b.y = (YT*)a.y + at * a.ldy;
+            if (a.scale) b.scale = a.scale + at;
+            hipLaunchKernelGGL((rmsnorm_kernel<XT, YT, NORM, decltype(v)::value, decltype(G)::value, decltype(P)::value>), dim3((unsigned)cdiv(b.rows, rows)),
+                               dim3(norm_threads(G)), 0, st, b);
+        }
     };
     if (a.width < V) go(int_c<1>(), int_c<8>(), int_c<1>());
     else for_row_shape<false>(cdiv(a.width, V), [&](auto G, auto P) { if constexpr (V * decltype(P)::value <= 32) go(int_c<V>(), G, P); });
