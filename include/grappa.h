@@ -593,6 +593,7 @@ grp_status grp_rmsnorm_backward(int64_t rows, int32_t width, const void* dy, int
 /* Workspace of the three products (DEV, 16-byte aligned, contents undefined); 0: none is needed.  dtype: of A and W.  It holds partial sums
  * and, for large products whose rows are no whole units of 16 bytes (N or K no multiple of 8, in e4m3 of 16), copies of the operands. */
 size_t     grp_linear_workspace_bytes(int32_t kind, int64_t M, int32_t N, int32_t K, int32_t dtype);
+/* Products of 2^31 rows or columns or more, or of 2^38 results, can be refused (GRP_EUNSUPPORTED).  Sums may be of any length. */
 /* z = A W + bias;  C = act(z) + r.
  *   dtype GRP_DTYPE_BF16:  A DEV [M x K], W DEV [K x N] (the layout of a model's parameters); no scales
  *   dtype GRP_DTYPE_E4M3:  A DEV [M x K], W DEV [N x K], row m of A times a_scale[m] and row n of W times w_scale[n]

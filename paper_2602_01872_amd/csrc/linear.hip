@@ -999,15 +999,16 @@ struct LinearPlan {
     bool tall = false;                  // linear_tall_kernel, whatever the alignment
     size_t packed_p = 0, packed_q = 0;  // bytes of the operands' copies as whole units (0: none)
     int64_t steps = 0, per_split = 0;
-    int32_t tiles_i = 0, tiles_j = 0, splits = 1, ld_part = 0;
+    int32_t tiles_j = 0, splits = 1, ld_part = 0;
     size_t bytes = 0;
 };
-constexpr int64_t MOST_TILES = (int64_t)1 << 30;
 // The tiles there are, and what a step of 128 bytes of one takes, in us, with one workgroup on a CU and with as many as fit there; what a tile takes
 // besides (measured on products of K = 64 .. 4096 over 128 .. 3e5 rows).
 struct TileShape { int i, j, most, threads; float step[3], besides; };
 constexpr TileShape LINEAR_TILES[] = {{64, 128, 3, 128, {0.50f, 0.55f, 0.78f}, 1.5f}, {128, 128, 2, 256, {0.62f, 0.95f, 0.f}, 2.f}, {256, 256, 1, 512, {1.6f, 0.f, 0.f}, 6.f}};
 constexpr int CUS = 256;
+// Whether a launch of so many workgroups of `threads` holds fewer than 2^32 work-items, which is the limit.
+bool launch_holds(double workgroups, int threads) { return workgroups * threads < 4294967296.0; }
 
 // The tile and the number of splits of the sums with the least time by a model of it: workgroups in rounds of what fits the CUs, 15 TB/s for the tiles' loads,
 // and for splits a second launch that reads the partial sums (1.5 us; two launches cost the host 9.5).  Against the best of all tiles and splits, on 90
@@ -1042,8 +1043,6 @@ double search_tiles(LinearPlan& p, int op, int64_t I, int32_t J, bool registers)
             }
         }
     }
-    p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[p.shape].i);
-    p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[p.shape].j);
     return best;
 }
 
@@ -1054,9 +1053,10 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
     // Few rows: one launch, as long as the sums are not so long that tiles in splits, two launches, are faster.  Forward of bf16, J = 4096, us, this and tiles:
     // 1 row, K = 4096 8.9 and 10.9, K = 8192 17.6 and 16.6; 32 rows, K = 2048 8.3 and 10.8, K = 4096 15.1 and 14.0; 64 rows, K = 1024 (J = 256) 7.0 and 9.3, K = 2048
     // (J = 1024) 11.0 and 10.0.
-    if (op != GRAD_W && I <= 64 && J >= 8 && s_bytes <= (I <= 16 ? 8 : I <= 32 ? 6 : 3) * 1024) {
+    const int few_columns = J <= 16 * CUS ? 1 : 2;
+    if (op != GRAD_W && I <= 64 && J >= 8 && s_bytes <= (I <= 16 ? 8 : I <= 32 ? 6 : 3) * 1024 && launch_holds((double)cdiv(J, 16 * few_columns), 64 * FEW_WAVES)) {
         p.few = I <= 16 ? 1 : I <= 32 ? 2 : 4;
-        p.few_columns = J <= 16 * CUS ? 1 : 2;
+        p.few_columns = few_columns;
         p.tiles_j = (int32_t)cdiv(J, 16 * p.few_columns);
         return p;
     }
@@ -1068,8 +1068,6 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
         p.splits = 1;
         p.shape = 1;                    // (rows of more than 256 that begin at odd elements are left to tiles, unsplit)
         p.per_split = p.steps;
-        p.tiles_i = (int32_t)cdiv(I, LINEAR_TILES[1].i);
-        p.tiles_j = (int32_t)cdiv(J, LINEAR_TILES[1].j);
         return p;
     };
     if (!odd_p && !odd_q) {
@@ -1108,73 +1106,122 @@ bool whole_units(const void* p, int64_t ld, int64_t n, int es) {
     return (uintptr_t)p % 16 == 0 && ld * es % 16 == 0 && n * es % 16 == 0 && ld * es < (1 << 22);
 }
 
+// How a product is made: the kernel and its launch, from sizes, pitches and alignment.
+enum LinearKind { FEW, TALL, TILES };
+struct LinearWay {
+    LinearPlan plan;
+    LinearKind kind = TILES;
+    bool units_p = false, units_q = false, pack = false;     // operands whose rows are whole units; whether the others are copied to such
+    bool dma = false;                    // tiles straight into LDS
+    int shape = 0;                       // of LINEAR_TILES
+    bool odd = false;                    // TALL: rows that are no whole dwords
+    int chunks = 0, kb = 0, blocks = 0;  //       of 64 bytes of s; of LDS; of 64 columns of a workgroup
+    double x = 0.0;                      // workgroups
+    int64_t y = 1;
+    int threads = 0;
+    bool fits = true;                    // a launch holds them
+};
+LinearWay way_of(int op, const LinearArgs& a) {
+    LinearWay w;
+    w.plan = plan_of(op, a.I, a.J, a.S);
+    const LinearPlan& p = w.plan;
+    if (p.few) {
+        w.kind = FEW;
+        w.x = p.tiles_j;
+        w.y = cdiv(a.I, 16 * p.few);
+        w.threads = 64 * FEW_WAVES;
+        return w;
+    }
+    const int es = elem_size(op);
+    w.units_p = whole_units(a.P, a.ldp, p_columns(op) ? a.I : a.S, es);
+    w.units_q = whole_units(a.Q, a.ldq, q_columns(op) ? a.J : a.S, es);
+    w.odd = (uintptr_t)a.P % 4 != 0 || a.ldp % 2 != 0;
+    if ((p.tall || (may_be_tall(op, a.S) && !(w.units_p && w.units_q) && !p.packed_p && !p.packed_q)) && (a.S <= 256 || !w.odd)) {
+        const int64_t walks = cdiv(cdiv(a.I, 16), TALL_WAVES);
+        w.chunks = a.S <= 64 ? 2 : a.S <= 128 ? 4 : a.S <= 256 ? 8 : 16;
+        const int block_kb = w.chunks / 2 * 8;
+        const int64_t columns = cdiv(a.J, 64);
+        // as much of W as fits, but a workgroup for every CU
+        w.blocks = (int)std::min<int64_t>(std::min<int64_t>(columns, 128 / block_kb), std::max<int64_t>(1, columns * std::min<int64_t>(walks, CUS) / CUS));
+        w.kb = w.blocks * block_kb <= 64 ? 64 : 128;
+        w.y = cdiv(columns, w.blocks);
+        w.x = (double)std::min<int64_t>(walks, round_up(cdiv((int64_t)CUS * (w.kb == 64 ? 2 : 1), w.y), 8));
+        w.threads = 64 * TALL_WAVES;
+        if (w.y <= 65535) {              // (more columns are left to tiles)
+            w.kind = TALL;
+            return w;
+        }
+        w.y = 1;
+    }
+    w.pack = (p.packed_p || p.packed_q) && (w.units_p || p.packed_p) && (w.units_q || p.packed_q);
+    w.dma = w.pack || (w.units_p && w.units_q);
+    w.shape = w.dma ? p.shape : 1;       // by way of registers: those of 128 x 128 tiles suffice
+    const TileShape& t = LINEAR_TILES[w.shape];
+    w.x = (double)cdiv(a.I, t.i) * (double)cdiv(a.J, t.j) * p.splits;
+    w.threads = t.threads;
+    w.fits = launch_holds(w.x, w.threads);
+    return w;
+}
+
 template <int OP> grp_status run_linear(const char* who, const char* name, LinearArgs a, double bytes, void* ws, size_t ws_bytes, hipStream_t st) {
     constexpr int ES = elem_size(OP);
-    const LinearPlan p = plan_of(OP, a.I, a.J, a.S);
-    if ((int64_t)p.tiles_i * p.tiles_j * p.splits > MOST_TILES) return fail(GRP_EUNSUPPORTED, "%s: too large", who);
+    const LinearWay w = way_of(OP, a);
+    const LinearPlan& p = w.plan;
+    if (!w.fits) return fail(GRP_EUNSUPPORTED, "%s: %lld x %d results are more than a launch holds", who, (long long)a.I, a.J);
     const size_t need = p.bytes + p.packed_p + p.packed_q;
     if (need && (!ws || ws_bytes < need)) return fail(GRP_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws ? ws_bytes : (size_t)0, need);
     if (need && (uintptr_t)ws % 16) return fail(GRP_EINVAL, "%s: workspace is not 16-byte aligned", who);
     const double flops = 2.0 * (double)a.I * a.J * a.S;
+    const dim3 grid((unsigned)w.x, (unsigned)w.y), group((unsigned)w.threads);
     if constexpr (OP != GRAD_W)
-        if (p.few) {
+        if (w.kind == FEW) {
             ProfScope ps(name, st, flops, bytes);
-            auto go = [&](auto kernel) { a.tiles_j = p.tiles_j; hipLaunchKernelGGL(kernel, dim3((unsigned)p.tiles_j, (unsigned)cdiv(a.I, 16 * p.few)), dim3(64 * FEW_WAVES), 0, st, a); };
+            auto go = [&](auto kernel) { a.tiles_j = p.tiles_j; hipLaunchKernelGGL(kernel, grid, group, 0, st, a); };
             if (p.few == 1) { if (p.few_columns == 1) go(linear_few_kernel<OP, 1, 1>); else go(linear_few_kernel<OP, 1, 2>); }
             else if (p.few == 2) { if (p.few_columns == 1) go(linear_few_kernel<OP, 2, 1>); else go(linear_few_kernel<OP, 2, 2>); }
             else { if (p.few_columns == 1) go(linear_few_kernel<OP, 4, 1>); else go(linear_few_kernel<OP, 4, 2>); }
             GRP_LAUNCH_CHECK();
             return GRP_OK;
         }
-    const int64_t length_p = p_columns(OP) ? a.I : a.S, length_q = q_columns(OP) ? a.J : a.S;
-    bool units_p = whole_units(a.P, a.ldp, length_p, ES), units_q = whole_units(a.Q, a.ldq, length_q, ES);
     if constexpr (OP == FWD_BF16 || OP == GRAD_X)
-        if (const bool odd = (uintptr_t)a.P % 4 != 0 || a.ldp % 2 != 0; (p.tall || (may_be_tall(OP, a.S) && !(units_p && units_q) && !p.packed_p && !p.packed_q)) && (a.S <= 256 || !odd)) {
+        if (w.kind == TALL) {
             ProfScope ps(name, st, flops, bytes);
-            const int64_t rows_16 = cdiv(a.I, 16), walks = cdiv(rows_16, TALL_WAVES);
-            const int chunks = a.S <= 64 ? 2 : a.S <= 128 ? 4 : a.S <= 256 ? 8 : 16, block_kb = chunks / 2 * 8;
-            const int columns = (int)cdiv(a.J, 64);
-            // as much of W as fits, but a workgroup for every CU
-            const int blocks = (int)std::min<int64_t>(std::min(columns, 128 / block_kb), std::max<int64_t>(1, columns * walks / CUS));
-            const int kb = blocks * block_kb <= 64 ? 64 : 128;
-            const int64_t groups = cdiv(columns, blocks), across = std::min<int64_t>(walks, round_up(cdiv((int64_t)CUS * (kb == 64 ? 2 : 1), groups), 8));
-            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)across, (unsigned)groups), dim3(64 * TALL_WAVES), 0, st, a, blocks, rows_16); };
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, group, 0, st, a, w.blocks, cdiv(a.I, 16)); };
             auto by_type = [&](auto c, auto lds) {
                 constexpr int C = decltype(c)::value, KB = decltype(lds)::value;
                 auto by_row = [&](auto o) {
                     if (a.c_bf16) go(linear_tall_kernel<OP, C, false, decltype(o)::value, KB>);
                     else go(linear_tall_kernel<OP, C, true, decltype(o)::value, KB>);
                 };
-                if (!odd) by_row(std::false_type());
+                if (!w.odd) by_row(std::false_type());
                 else if constexpr (C <= 8) by_row(std::true_type());
             };
             auto by_lds = [&](auto c) {
-                if (kb == 64) by_type(c, std::integral_constant<int, 64>());
+                if (w.kb == 64) by_type(c, std::integral_constant<int, 64>());
                 else by_type(c, std::integral_constant<int, 128>());
             };
-            if (chunks == 2) by_lds(std::integral_constant<int, 2>());
-            else if (chunks == 4) by_lds(std::integral_constant<int, 4>());
-            else if (chunks == 8) by_lds(std::integral_constant<int, 8>());
+            if (w.chunks == 2) by_lds(std::integral_constant<int, 2>());
+            else if (w.chunks == 4) by_lds(std::integral_constant<int, 4>());
+            else if (w.chunks == 8) by_lds(std::integral_constant<int, 8>());
             else by_lds(std::integral_constant<int, 16>());
             GRP_LAUNCH_CHECK();
             return GRP_OK;
         }
+    const int64_t length_p = p_columns(OP) ? a.I : a.S, length_q = q_columns(OP) ? a.J : a.S;
     a.end_p = (((p_columns(OP) ? a.S : a.I) - 1) * a.ldp + length_p) * ES;
     a.end_q = (((q_columns(OP) ? a.S : a.J) - 1) * a.ldq + length_q) * ES;
-    if ((p.packed_p || p.packed_q) && (units_p || p.packed_p) && (units_q || p.packed_q)) {
+    if (w.pack) {
         char* at = (char*)ws + p.bytes;
         PackOperand o[2] = {};
-        auto copy = [&](PackOperand& k, const void*& from, int64_t& ld, int64_t& end, bool columns, int64_t O, int64_t length, size_t size, bool& units) {
-            if (units) return;
+        auto copy = [&](PackOperand& k, const void*& from, int64_t& ld, int64_t& end, bool columns, int64_t O, int64_t length, size_t size) {
             k = PackOperand{from, ld, columns ? a.S : O, length, at, cdiv(length * ES, 16)};
             from = at;
             ld = k.units * 16 / ES;
             end = k.rows * k.units * 16;
             at += size;
-            units = true;
         };
-        copy(o[0], a.P, a.ldp, a.end_p, p_columns(OP), a.I, length_p, p.packed_p, units_p);
-        copy(o[1], a.Q, a.ldq, a.end_q, q_columns(OP), a.J, length_q, p.packed_q, units_q);
+        if (!w.units_p) copy(o[0], a.P, a.ldp, a.end_p, p_columns(OP), a.I, length_p, p.packed_p);
+        if (!w.units_q) copy(o[1], a.Q, a.ldq, a.end_q, q_columns(OP), a.J, length_q, p.packed_q);
         const int64_t all = o[0].rows * o[0].units + o[1].rows * o[1].units;
         if (all > 0) {
             ProfScope ps("linear_pack", st, 0.0, 32.0 * all);
@@ -1186,22 +1233,14 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
     a.splits = p.splits;
     a.ld_part = p.ld_part;
     a.steps_per_split = p.per_split;
-    a.tiles_i = p.tiles_i;
-    a.tiles_j = p.tiles_j;
-    const bool dma = units_p && units_q;
-    if (!dma) {                         // by way of registers: those of 128 x 128 tiles suffice
-        a.tiles_i = (int32_t)cdiv(a.I, LINEAR_TILES[1].i);
-        a.tiles_j = (int32_t)cdiv(a.J, LINEAR_TILES[1].j);
-        if ((int64_t)a.tiles_i * a.tiles_j * p.splits > MOST_TILES) return fail(GRP_EUNSUPPORTED, "%s: too large", who);
-    }
+    a.tiles_i = (int32_t)cdiv(a.I, LINEAR_TILES[w.shape].i);
+    a.tiles_j = (int32_t)cdiv(a.J, LINEAR_TILES[w.shape].j);
     {
         ProfScope ps(name, st, flops, bytes);
-        auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles_i * a.tiles_j * p.splits)), dim3((unsigned)LINEAR_TILES[dma ? p.shape : 1].threads), 0, st, a);
-        };
-        if (!dma) go(linear_kernel<OP, 2, 2, 4, false>);
-        else if (p.shape == 0) go(linear_kernel<OP, 1, 2, 4, true>);
-        else if (p.shape == 1) go(linear_kernel<OP, 2, 2, 4, true>);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, group, 0, st, a); };
+        if (!w.dma) go(linear_kernel<OP, 2, 2, 4, false>);
+        else if (w.shape == 0) go(linear_kernel<OP, 1, 2, 4, true>);
+        else if (w.shape == 1) go(linear_kernel<OP, 2, 2, 4, true>);
         else go(linear_kernel<OP, 2, 4, 8, true>);
         GRP_LAUNCH_CHECK();
     }
@@ -1217,6 +1256,25 @@ template <int OP> grp_status run_linear(const char* who, const char* name, Linea
     }
     return GRP_OK;
 }
+
+}  // namespace
+// What a product D[I x J] with sums of S runs as, as numbers: op is a LinearOp; out: kind, then few: fragments of rows and of columns, tall: chunks, odd rows
+// and LDS, tiles: shape (3: by way of registers), splits and copied operands; then workgroups, the second dimension's, and threads.  False: refused.
+bool linear_way(int op, int64_t I, int32_t J, int64_t S, const void* P, int64_t ldp, const void* Q, int64_t ldq, int64_t (&out)[7]) {
+    LinearArgs a = {};
+    a.P = P; a.ldp = ldp; a.Q = Q; a.ldq = ldq; a.I = I; a.J = J; a.S = S;
+    const LinearWay w = way_of(op, a);
+    const bool few = w.kind == FEW, tall = w.kind == TALL;
+    out[0] = w.kind;
+    out[1] = few ? w.plan.few : tall ? w.chunks : w.dma ? w.shape : 3;
+    out[2] = few ? w.plan.few_columns : tall ? w.odd : w.plan.splits;
+    out[3] = few ? 0 : tall ? w.kb : w.pack;
+    out[4] = w.fits ? (int64_t)w.x : -1;
+    out[5] = w.y;
+    out[6] = w.threads;
+    return w.fits;
+}
+namespace {
 
 bool aligned_to(const void* p, int32_t dtype) { return dtype == GRP_DTYPE_E4M3 || (uintptr_t)p % (dtype == GRP_DTYPE_BF16 ? 2 : 4) == 0; }
 grp_status check_sizes(const char* who, int64_t m, int32_t n, int32_t k) {

@@ -48,3 +48,25 @@ def test_wide_rows(g):
     assert bool((bits == torch.tensor(0xFE7E - 0x10000, device=DEV, dtype=torch.int16)).all())
     del x, q, bits
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,n,k,act", [(2, 134_300_000, 8, "ACT_NONE"), (66, 67_200_001, 9, "ACT_RELU")])
+def test_layers_of_many_columns(g, rows, n, k, act):
+    """More columns than the kernel for few rows, or the one that keeps W in LDS, has workgroups for: tiles.  Whole numbers, so that every sum is exact."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("60 GB of device memory are needed")
+    r = torch.Generator(device=DEV)
+    r.manual_seed(3)
+    a = torch.randint(-4, 5, (rows, k), generator=r, device=DEV).to(torch.bfloat16)
+    w = torch.randint(-4, 5, (k, n), generator=r, device=DEV, dtype=torch.int8).to(torch.bfloat16)
+    c = torch.full((rows, n), 0.5, device=DEV, dtype=torch.bfloat16)
+    need = g.grp_linear_workspace_bytes(g.LINEAR_FORWARD, rows, n, k, g.DTYPE_BF16)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
+    g.grp_linear(rows, n, k, a, k, w, n, g.DTYPE_BF16, None, None, None, getattr(g, act), None, 0, c, n, g.DTYPE_BF16, None, 0, ws)
+    for at in range(0, n, 1 << 25):
+        want = a.float() @ w[:, at:at + (1 << 25)].float()
+        want = want.relu() if act == "ACT_RELU" else want
+        assert torch.equal(c[:, at:at + (1 << 25)].float(), want)          # at most 144: bf16 holds it
+    del a, w, c, ws, want
+    torch.cuda.empty_cache()
