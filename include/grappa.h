@@ -584,7 +584,7 @@ grp_status grp_rmsnorm_backward(int64_t rows, int32_t width, const void* dy, int
                                 void* dh, int64_t lddh, float* dweight, void* workspace, size_t workspace_bytes, void* stream);
 
 #define GRP_ACT_NONE 0
-#define GRP_ACT_RELU 1
+#define GRP_ACT_RELU 1           /* max(z, 0), slope 1 where z > 0, else 0; both NaN for NaN    */
 #define GRP_ACT_GELU 2           /* z Phi(z), Phi the normal distribution's (erf)           */
 #define GRP_ACT_SILU 3           /* z / (1 + exp(-z))                                        */
 #define GRP_LINEAR_FORWARD 0

@@ -82,7 +82,7 @@ __device__ __forceinline__ float normal_tail(float z, float& e) {
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f)); }
 
 template <int ACT> __device__ __forceinline__ float act_of(float z) {
-    if constexpr (ACT == GRP_ACT_RELU) return z > 0.f ? z : 0.f;
+    if constexpr (ACT == GRP_ACT_RELU) return z <= 0.f ? 0.f : z;              // (NaN stays)
     if constexpr (ACT == GRP_ACT_GELU) {
         float e;
         const float q = normal_tail(z, e);
@@ -92,7 +92,7 @@ template <int ACT> __device__ __forceinline__ float act_of(float z) {
     return z;
 }
 template <int ACT> __device__ __forceinline__ float slope_of(float z) {
-    if constexpr (ACT == GRP_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == GRP_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     if constexpr (ACT == GRP_ACT_GELU) {
         float e;
         const float q = normal_tail(z, e);

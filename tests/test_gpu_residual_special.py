@@ -1,0 +1,101 @@
+"""Infinities and NaN through the layers' activations and slopes, on every way a product takes."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16 = torch.bfloat16
+INF, NAN = float("inf"), float("nan")
+# rows, columns, sums: one row, few rows, tiles of whole units and of others, W in LDS, copied operands
+SIZES = [(1, 40, 16), (40, 24, 64), (300, 136, 520), (300, 137, 521), (9000, 72, 64), (9000, 71, 65), (2000, 1030, 1021)]
+ACTS = ["ACT_NONE", "ACT_RELU", "ACT_GELU", "ACT_SILU"]
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_2602_01872_amd as lib
+    lib.load()
+    return lib
+
+
+def value(z, act):
+    """The header's formulas in 64 bits, with infinities and NaN as the arithmetic has them."""
+    if act == "ACT_RELU":
+        return torch.maximum(z, torch.zeros_like(z))
+    if act == "ACT_GELU":
+        return z * 0.5 * torch.erfc(-z * math.sqrt(0.5))
+    if act == "ACT_SILU":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def slope(z, act):
+    if act == "ACT_RELU":
+        return torch.where(z.isnan(), z, (z > 0).double())
+    if act == "ACT_GELU":
+        return 0.5 * torch.erfc(-z * math.sqrt(0.5)) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    if act == "ACT_SILU":
+        s = 1 / (1 + torch.exp(-z))
+        return s * (1 + z * (1 - s))
+    return torch.ones_like(z)
+
+
+def alike(got, want, tol):
+    got, want = got.double(), want.double()
+    assert torch.equal(got.isnan(), want.isnan())
+    inf = want.isinf()
+    assert torch.equal(got[inf], want[inf]) and torch.equal(got.isinf(), inf)
+    ok = want.isfinite()
+    assert bool(((got - want).abs()[ok] <= tol.expand_as(want)[ok]).all())
+
+
+def workspace(g, kind, m, n, k, dtype):
+    b = g.grp_linear_workspace_bytes(kind, m, n, k, dtype)
+    return torch.empty(b, dtype=torch.uint8, device=DEV) if b else None
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_activations(g, m, n, k, act, kind):
+    """The bias brings them: column 0 infinite, 1 minus infinite, 2 NaN; A's first row brings a NaN to all columns.  A and W hold small whole numbers, so z is exact."""
+    r = torch.Generator(device=DEV)
+    r.manual_seed(m + n)
+    e8 = kind == "e4m3"
+    t = torch.float8_e4m3fn if e8 else BF16
+    a = torch.randint(-1, 2, (m, k), generator=r, device=DEV).float()
+    w = torch.randint(-1, 2, (k, n), generator=r, device=DEV).float() * (torch.rand(k, n, generator=r, device=DEV) < 4 / k)
+    a[0, k // 2] = NAN
+    bias = torch.zeros(n, device=DEV)
+    bias[:3] = torch.tensor([INF, -INF, NAN])
+    z64 = a.double() @ w.double() + bias.double()
+    z64[0] = NAN
+    aq, wq = a.to(t), (w.t().contiguous() if e8 else w).to(t)
+    for ct, code in ((torch.float32, g.DTYPE_FP32), (BF16, g.DTYPE_BF16)):
+        c, z = torch.full((m, n), 7.5, device=DEV, dtype=ct), torch.full((m, n), 7.5, device=DEV, dtype=BF16)
+        dt = g.DTYPE_E4M3 if e8 else g.DTYPE_BF16
+        g.grp_linear(m, n, k, aq, k, wq, k if e8 else n, dt, None, None, bias, getattr(g, act), None, 0, c, n, code, z, n, workspace(g, 0, m, n, k, dt))
+        want = value(z64, act)
+        alike(c, want, want.abs() * torch.finfo(ct).eps / 2 * 1.01 + (1 + z64.abs()) * 2.0 ** -20)
+        alike(z, z64, z64.abs() * 2.0 ** -8)
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_slopes(g, m, n, k, act):
+    """The pre-activation brings them: sizes as above, n and k in each other's place."""
+    r = torch.Generator(device=DEV)
+    r.manual_seed(m + n)
+    dz = torch.randint(1, 3, (m, k), generator=r, device=DEV).float()
+    w = (torch.rand(n, k, generator=r, device=DEV) < 4 / k).float()
+    w[:, 0] = 1                                       # no sum is zero
+    zin = torch.randn(m, n, generator=r, device=DEV).to(BF16)
+    zin[:, 0], zin[:, 1], zin[:, 2] = INF, -INF, NAN
+    lin = dz.double() @ w.double().t()
+    want = lin * slope(zin.double(), act)
+    for dt, code in ((torch.float32, g.DTYPE_FP32), (BF16, g.DTYPE_BF16)):
+        da = torch.full((m, n), 7.5, device=DEV, dtype=dt)
+        g.grp_linear_dx(m, k, n, dz.to(BF16), k, w.to(BF16), k, getattr(g, act), zin, n, da, n, code, workspace(g, 1, m, k, n, g.DTYPE_BF16))
+        alike(da, want, want.abs() * torch.finfo(dt).eps / 2 * 1.01 + lin.abs() * (1 + zin.double().abs()) * 2.0 ** -20)
