@@ -366,15 +366,17 @@ __global__ __launch_bounds__(norm_threads(G)) void rmsnorm_grad_kernel(NormGradA
             sd = row_reduce<G>(sd, add, (float*)nullptr);
         }
         const float rho = rsqrtf(ss / (float)a.width + a.eps);
-        const float k = rho * rho * rho * (sd / (float)a.width);
+        // dh = rho (u - v mean(u v)) + g, v = h rho: rho^3 leaves fp32's range where |h| is 10^13 or 10^-13 and its product with h mean(u h) does not
+        const float k = rho * (rho * (sd / (float)a.width));
         HT* out = (HT*)a.dh + row * a.lddh;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                dw[p][e] = e >= at[p].skip ? fmaf(d[p][e], h[p][e] * rho, dw[p][e]) : 0.f;
-                o[e] = fmaf(-h[p][e], k, rho * (d[p][e] * w[p][e])) + t[p][e];
+                const float v = h[p][e] * rho;
+                dw[p][e] = e >= at[p].skip ? fmaf(d[p][e], v, dw[p][e]) : 0.f;
+                o[e] = fmaf(-v, k, rho * (d[p][e] * w[p][e])) + t[p][e];
             }
             if (at[p].skip < V) store_v<V>(out + at[p].at, o);
         }

@@ -99,3 +99,43 @@ def test_slopes(g, m, n, k, act):
         da = torch.full((m, n), 7.5, device=DEV, dtype=dt)
         g.grp_linear_dx(m, k, n, dz.to(BF16), k, w.to(BF16), k, getattr(g, act), zin, n, da, n, code, workspace(g, 1, m, k, n, g.DTYPE_BF16))
         alike(da, want, want.abs() * torch.finfo(dt).eps / 2 * 1.01 + lin.abs() * (1 + zin.double().abs()) * 2.0 ** -20)
+
+
+def norm_gradient(g, dy, h, w, eps, add=None):
+    rows, width = h.shape
+    dh, dw = torch.empty_like(h), torch.empty(width, device=DEV)
+    ws = torch.empty(g.grp_rmsnorm_backward_workspace_bytes(rows, width), dtype=torch.uint8, device=DEV)
+    code = lambda t: g.DTYPE_FP32 if t.dtype is torch.float32 else g.DTYPE_BF16
+    g.grp_rmsnorm_backward(rows, width, dy, width, code(dy), h, width, code(h), w, eps, add, width, dh, width, dw, ws)
+    return dh, dw
+
+
+@pytest.mark.parametrize("width", [3, 8, 100, 300, 1003, 5000])
+@pytest.mark.parametrize("size,eps", [(1e15, 1e-6), (1e17, 1e-6), (1e-15, 0.0), (1e-15, 1e-30), (1.0, 1e-6)])
+@pytest.mark.parametrize("ht", [torch.float32, BF16])
+def test_norm_gradient_of_large_and_small_rows(g, width, size, eps, ht):
+    """The result is of dy / |h|'s size, which fp32 holds, though |h|^-3 is none of its numbers.  Sums of at most 48 terms a lane and tree, as everywhere: (2 x 48 + 12) 2^-24."""
+    r = torch.Generator(device=DEV)
+    r.manual_seed(width)
+    h = (torch.randn(7, width, generator=r, device=DEV) * size).to(ht)
+    dy = torch.randn(7, width, generator=r, device=DEV)
+    w = 1 + 0.3 * torch.randn(width, generator=r, device=DEV)
+    dh, dw = norm_gradient(g, dy, h, w, eps)
+    H, U = h.double(), (dy * 1.0).double() * w.double()
+    rho = 1 / torch.sqrt(H.square().mean(1, keepdim=True) + eps)
+    v = H * rho
+    want = rho * (U - v * (U * v).mean(1, keepdim=True))
+    scale = rho * (U.abs() + v.abs() * (U * v).abs().mean(1, keepdim=True))
+    assert bool(dh.isfinite().all())
+    assert bool(((dh.double() - want).abs() <= want.abs() * torch.finfo(ht).eps / 2 + scale * 108 * 2.0 ** -24).all())
+    assert bool(((dw.double() - (dy.double() * v).sum(0)).abs() <= (dy.double() * v).abs().sum(0) * 75 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("width", [3, 8, 300, 5000])
+def test_norm_gradient_of_rows_of_zeros(g, width):
+    """rho u, and nothing else: with the smallest eps whose root is a number, too."""
+    h, dy = torch.zeros(5, width, device=DEV), torch.randn(5, width, device=DEV)
+    for eps in (1e-6, 1e-30, 1e-37):
+        dh, dw = norm_gradient(g, dy, h, None, eps)
+        want = dy.double() / math.sqrt(eps)
+        assert bool(((dh.double() - want).abs() <= want.abs() * 4 * 2.0 ** -24).all()) and bool((dw == 0).all())
