@@ -1311,6 +1311,7 @@ extern "C" grp_status grp_linear(int64_t m, int32_t n, int32_t k, const void* a,
     if (!aligned_to(a, dtype) || !aligned_to(w, dtype) || !aligned_to(c, c_dtype) || !aligned_to(r, c_dtype) || !aligned_to(z, GRP_DTYPE_BF16) ||
         !aligned_to(bias, GRP_DTYPE_FP32) || !aligned_to(a_scale, GRP_DTYPE_FP32) || !aligned_to(w_scale, GRP_DTYPE_FP32))
         return fail(GRP_EINVAL, "grp_linear: a pointer is not aligned to its elements");
+    if (m > 1 && r == c && ldr != ldc) return fail(GRP_EINVAL, "grp_linear: C in place of r needs its pitch");
     LinearArgs x = {};
     x.P = a; x.ldp = lda; x.Q = w; x.ldq = ldw; x.I = m; x.J = n; x.S = k;
     x.a_scale = a_scale; x.w_scale = w_scale; x.bias = bias; x.act = act; x.r = r; x.ldr = ldr;

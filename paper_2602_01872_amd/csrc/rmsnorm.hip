@@ -501,6 +501,7 @@ extern "C" grp_status grp_rmsnorm(int64_t rows, int32_t width, const void* x, in
     if (off_grid(x, x_dtype) || off_grid(r, x_dtype) || off_grid(h, x_dtype) || off_grid(y, y_dtype) || off_grid(weight, GRP_DTYPE_FP32) ||
         (y_dtype == GRP_DTYPE_E4M3 && off_grid(scale, GRP_DTYPE_FP32)))
         return fail(GRP_EINVAL, "grp_rmsnorm: a pointer is not aligned to its elements");
+    if (rows > 1 && h && ((h == x && ldh != ldx) || (h == r && ldh != ldr))) return fail(GRP_EINVAL, "grp_rmsnorm: h in place of x or r needs its pitch");
     NormArgs a{rows, width, x, ldx, r, ldr, weight, eps, h, ldh, y, ldy, scale};
     ProfScope ps("rmsnorm", (hipStream_t)stream, 6.0 * rows * width,
                  (double)rows * width * (bytes_of(x_dtype) * (1 + (r ? 1 : 0) + (h ? 1 : 0)) + bytes_of(y_dtype)));
@@ -541,6 +542,7 @@ extern "C" grp_status grp_rmsnorm_backward(int64_t rows, int32_t width, const vo
     if (off_grid(dy, dy_dtype) || off_grid(h, h_dtype) || off_grid(g, h_dtype) || off_grid(dh, h_dtype) || off_grid(weight, GRP_DTYPE_FP32) ||
         off_grid(dweight, GRP_DTYPE_FP32) || (dweight && off_grid(workspace, GRP_DTYPE_FP32)))
         return fail(GRP_EINVAL, "grp_rmsnorm_backward: a pointer is not aligned to its elements");
+    if (rows > 1 && ((dh == h && lddh != ldh) || (dh == g && lddh != ldg))) return fail(GRP_EINVAL, "grp_rmsnorm_backward: dh in place of h or g needs its pitch");
     const GradPlan p = grad_plan(rows, width, dy_dtype == GRP_DTYPE_BF16 && h_dtype == GRP_DTYPE_BF16);
     if (dweight && (!workspace || workspace_bytes < grad_part_bytes(p)))
         return fail(GRP_EWORKSPACE, "grp_rmsnorm_backward: workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, grad_part_bytes(p));
