@@ -22,6 +22,7 @@ struct ClipPiece {              // a run of one tensor's elements
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_WGS_MOST = 2048;           // partial sums that every workgroup of the second launch reads: eight a thread
 constexpr int64_t CLIP_PIECE_LEAST = 2048;    // elements of a piece: eight a thread
+constexpr int64_t CLIP_ELEMENTS_MOST = (int64_t)1 << 38;      // more than the memory of a GPU in the narrowest type
 
 }  // namespace
 }  // namespace grp
@@ -143,6 +144,7 @@ extern "C" grp_status grp_gradients_create(int32_t tensors, const void* const* s
         if (counts[i] > 0 && (!src[i] || (dst && !dst[i]))) return fail(GRP_EINVAL, "grp_gradients_create: tensor %d is null", i);
         const size_t el = dtypes[i] == GRP_DTYPE_BF16 ? 2 : 4;
         if ((uintptr_t)src[i] % el || (dst && (uintptr_t)dst[i] % el)) return fail(GRP_EINVAL, "grp_gradients_create: tensor %d is not aligned to its elements", i);
+        if (counts[i] > CLIP_ELEMENTS_MOST - total) return fail(GRP_EUNSUPPORTED, "grp_gradients_create: more than 2^38 elements");
         total += counts[i];
         bytes += (double)el * counts[i];
     }
