@@ -3,7 +3,8 @@ the operators of residual blocks (``grappa.h``).
 
 A block is pre-norm:  h = x + r,  out = h + act(norm(h) W1 + b1) W2 + b2, where r is the block's own output of before (the norm adds it).
 Activations and the weights' copies are bf16, master weights, gradients and the optimizer's moments fp32 (one flat vector each, as
-``grp_optimizer_step`` takes them).  ``serve`` runs the products in 8 bits, with weights quantized once.
+``grp_optimizer_step`` takes them): h, each block's output and the gradient that runs through them are rounded to bf16 at every block.  ``serve`` runs the products in
+8 bits, with weights quantized once, by the 8-bit matrix instructions, whose sums are shorter than fp32 (``grp_linear`` in ``grappa.h``).
 
 Parameters are set by writing into ``theta`` or its views ``params``: the next ``forward`` or ``serve`` makes the weights' copies anew.  That goes by torch's own
 count of writes, which a kernel of the user's own, a collective, a replayed graph and ``.data`` pass by: ``refresh()`` has to follow these.  A captured pass
