@@ -139,3 +139,18 @@ def test_norm_gradient_of_rows_of_zeros(g, width):
         dh, dw = norm_gradient(g, dy, h, None, eps)
         want = dy.double() / math.sqrt(eps)
         assert bool(((dh.double() - want).abs() <= want.abs() * 4 * 2.0 ** -24).all()) and bool((dw == 0).all())
+
+
+def test_tail_of_gelu(g):
+    """Relative error of z Phi(z) below zero.  The exponent z^2 / 2 is rounded three times (2.5 2^-24 of it, 7.5e-8 z^2 of the result); the reciprocal (an ulp and a half, up
+    to 2.7 times as much of the result), the exponential (an ulp), the polynomial's fit and its steps, and three products add up to less than 1.2e-6."""
+    z = torch.cat([-torch.logspace(-6, 0, 2000), torch.linspace(-13, -1, 20001)]).to(DEV)
+    n = z.numel()
+    a, w, c = torch.zeros(1, 1, device=DEV, dtype=BF16), torch.zeros(1, n, device=DEV, dtype=BF16), torch.empty(1, n, device=DEV)
+    g.grp_linear(1, n, 1, a, 1, w, n, g.DTYPE_BF16, None, None, z, g.ACT_GELU, None, 0, c, n, g.DTYPE_FP32, None, 0, workspace(g, 0, 1, n, 1, g.DTYPE_BF16))
+    want = z.double() * 0.5 * torch.erfc(-z.double() * math.sqrt(0.5))
+    rel = (c[0].double() / want - 1).abs()
+    for lo, hi in ((0, 1), (1, 4), (4, 5), (5, 8), (8, 10), (10, 13)):
+        part = (z.abs() >= lo) & (z.abs() <= hi)
+        print(f"|z| {lo} .. {hi}: {float(rel[part].max()):.1e}")
+    assert bool((rel <= 1.2e-6 + 7.5e-8 * z.double().square()).all())
