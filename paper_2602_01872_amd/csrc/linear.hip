@@ -327,7 +327,8 @@ __device__ __forceinline__ u32x4_al load_unit(const void* base, int64_t ld, int6
 // 16 bytes a lane from buffer `rsrc` at `off` to LDS, a wavefront's 64 places in a row from byte `lds` on.  (Inline: the compiler would wait for it before
 // any other read of LDS.  No register is written; who reads the tile waits for vmcnt(0) before the barrier that is before it.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, __amdgpu_buffer_rsrc_t rsrc, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
+    uint32_t m0;                     // (written in here: nothing that the compiler keeps in m0 outlives this)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds" : "={m0}"(m0) : "s"(lds), "v"(off), "s"(rsrc) : "memory");
 }
 
 // 16 e4m3 numbers in bf16 (exact).
