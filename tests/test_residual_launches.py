@@ -4,6 +4,8 @@ import os
 
 import pytest
 
+from tests._ways import OPS, way
+
 
 @pytest.fixture(scope="module")
 def lib():
@@ -26,21 +28,6 @@ def test_rows_of_a_norm_fit_a_launch(lib, lanes):
 
 
 P = 0x1000          # an address that is never used
-KINDS = ("few", "tall", "tiles")
-OPS = ("bf16", "e4m3", "e4m3 to fp32", "dx", "dw")
-
-
-def way(lib, op, i, j, s, pad=0, off=0):
-    """(accepted, kind, its three numbers, workgroups, of the second dimension, threads) of a product of i x j results, sums of s, rows `pad` elements apart."""
-    fn = getattr(lib, "_ZN3grp10linear_wayEililPKvlS1_lRA7_l")
-    fn.argtypes, fn.restype = [C.c_int, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(C.c_int64)], C.c_bool
-    out = (C.c_int64 * 7)()
-    es = 1 if op in ("e4m3", "e4m3 to fp32") else 2
-    length_p = i if op == "dw" else s
-    length_q = j if op in ("dw", "bf16") else s
-    ok = fn(OPS.index(op), i, j, s, P + off * es, length_p + pad, P + off * es, length_q + pad, out)
-    return ok, KINDS[out[0]], tuple(out[1:4]), out[4], out[5], out[6]
-
 
 @pytest.mark.parametrize("op", OPS)
 def test_launches_of_products_hold_less_than_the_limit(lib, op):
