@@ -166,3 +166,25 @@ def test_way(g, op, i, j, s, pad, off):
         by_weight(g, i, j, s, pad, off)
     else:
         forward(g, op, i, j, s, pad, off)
+
+
+def test_rows_that_begin_past_32_bits(g):
+    """2.3e9 elements of A: sums over all rows, first and last columns of the result, and first and last rows of the forward product."""
+    m, k, n = 140_001, 16_384, 16
+    r = torch.Generator(device=DEV)
+    r.manual_seed(1)
+    a = torch.empty(m, k, device=DEV, dtype=BF16)
+    for i in range(0, m, 20_000):
+        a[i:i + 20_000] = torch.randn(min(20_000, m - i), k, generator=r, device=DEV)
+    dz, w = draw(r, m, n).to(BF16), draw(r, k, n, k ** -0.5).to(BF16)
+    dw, c = torch.empty(k, n, device=DEV), torch.empty(m, n, device=DEV)
+    g.grp_linear_dw(m, n, k, a, k, dz, n, dw, n, None, room(g, g.LINEAR_DW, m, n, k, g.DTYPE_BF16))
+    for at in (slice(0, 64), slice(8192, 8256), slice(k - 64, k)):
+        A, D = a[:, at].double(), dz.double()
+        size = (A.square().t() @ D.square()).sqrt()
+        check(dw[at], A.t() @ D, size * 6 * sum_error(m), float(size.norm()) * sum_error(m), FP32)
+    g.grp_linear(m, n, k, a, k, w, n, g.DTYPE_BF16, None, None, None, g.ACT_NONE, None, 0, c, n, g.DTYPE_FP32, None, 0, room(g, g.LINEAR_FORWARD, m, n, k, g.DTYPE_BF16))
+    for at in (slice(0, 300), slice(131_000, 131_300), slice(m - 300, m)):
+        A, W = a[at].double(), w.double()
+        size = (A.square() @ W.square()).sqrt()
+        check(c[at], A @ W, size * 6 * sum_error(k), float(size.norm()) * sum_error(k), FP32)

@@ -1,11 +1,12 @@
-"""The sizes at which the linear layers are tested take every way that there is (CPU)."""
+"""The sizes at which the linear layers are tested take every way that there is, and the tests' bounds see a lost part of a sum (CPU)."""
 import math
 import os
 import random
 
 import pytest
+import torch
 
-from tests._ways import OPS, WAYS, way_class
+from tests._ways import OPS, WAYS, sum_error, way_class
 
 
 @pytest.fixture(scope="module")
@@ -43,3 +44,16 @@ def test_the_largest_tile_is_tested_at_odd_and_even_numbers_of_steps(lib, op, st
             assert i % 256 and j % 256
             seen.add((min(-(-s // step), 6 - -(-s // step) % 2), s % step == 0))
     assert {n for n, _ in seen} >= {1, 2, 3, 4, 5} and {whole for _, whole in seen} == {True, False}
+
+
+@pytest.mark.parametrize("i,j,s,splits", [(16, 24, 20_001, 64), (130, 70, 40_000, 128)])
+def test_the_bound_sees_a_lost_split(i, j, s, splits):
+    r = torch.Generator().manual_seed(3)
+    a, b = (torch.randn(s, n, generator=r).to(torch.bfloat16).double() for n in (i, j))
+    want, size = a.t() @ b, (a.square().t() @ b.square()).sqrt()
+    each = -(-s // splits)
+    parts = [(a[k:k + each].float().t() @ b[k:k + each].float()).double() for k in range(0, s, each)]
+    bound = sum_error(s) * float(size.norm())
+    assert float((sum(parts) - want).norm()) <= bound
+    for wrong in (sum(parts[:-1]), sum(parts) + parts[0], torch.zeros_like(want)):
+        assert float((wrong - want).norm()) > 20 * bound
