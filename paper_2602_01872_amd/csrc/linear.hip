@@ -6,7 +6,7 @@
 //
 // The 8-bit matrix instructions cut, of every eight products, what is below 2^-13 of the largest (measured on single instructions; rms 1.3e-5 of the
 // result on normal deviates).  Beside the rounding of a bf16 result (rms 1.6e-3) that is nothing, and they run at twice the rate; for fp32 results
-// e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those.
+// e4m3 numbers are widened to bf16, which holds them exactly, and multiplied as those (8192^3 384 us and 717, 4096^3 56 and 105).
 //
 // All are D[i, j] = sum_s P(i, s) Q(s, j): an operand either has s contiguous ("rows": A, dZ, the 8-bit weights) or its output index ("columns": W of the
 // forward product, both operands of dw).  Products are accumulated in fp32 by the matrix unit.  Three kernels make them: tiles (linear_kernel, with
@@ -19,8 +19,8 @@
 //   columns  LDS row s has the tile's output indices; ds_read_b64_tr_b16 turns four rows of 16 around into a lane's four consecutive s
 // Places are permuted by some bits of the row (swizzle) so that the 16 lanes of a group read different banks.
 //   The instruction's rows are D's columns: lane (g, t) holds D[i + t, j + 16 g + 4 f + e], e < 4, for the wavefront's fragments f < 4: 16 consecutive columns.
-//   Measured, 8192^3 with inputs that stay in the caches: forward 780 us (1410 TFLOP/s), dx 770 (1430), dw 800 (1370), 8 bits 370 (2990); the matrix unit is busy
-// 60 - 68 % of the cycles, a third of the rest goes to the loads (660 us without any), 256 x 256 tiles against 128 x 128: 790 and 1040 us (forward).
+//   Measured, 8192^3 with inputs that stay in the caches, on several cards: forward 770 - 800 us (1370 - 1430 TFLOP/s), dx 780 - 810, dw 800, 8 bits 370 - 385 (2860 - 2990);
+// the matrix unit is busy 53 - 68 % of the cycles, a third of the rest goes to the loads (660 us without any), 256 x 256 tiles against 128 x 128: 790 and 1040 us (forward).
 #include "common.h"
 
 namespace grp {
@@ -361,7 +361,6 @@ __device__ __forceinline__ void tile_of(unsigned b, unsigned all, int tiles_i, i
     tj = (int)(in / rows);
 }
 
-// DMA: rows of both operands are whole units of 16 bytes and begin on them.
 // What a lane reads of a fragment at once: all 128 bytes of s (its part: 32) for the 8-bit instruction, else half of them.
 template <int OP> using FragOf = std::conditional_t<OP == FWD_E4M3, intx8, u32x4_al>;
 template <int OP> __device__ __forceinline__ void multiply(const FragOf<OP>& q, const FragOf<OP>& p, floatx4& c) {
@@ -376,6 +375,7 @@ template <int OP> __device__ __forceinline__ void multiply(const FragOf<OP>& q, 
     }
 }
 
+// DMA: rows of both operands are whole units of 16 bytes and begin on them.
 template <int OP, int WI, int WJ, int FI, bool DMA> __global__ __launch_bounds__(64 * WI * WJ, 2) void linear_kernel(LinearArgs a) {
     constexpr int ES = elem_size(OP), NT = 64 * WI * WJ, TI = 16 * FI * WI, TJ = 64 * WJ, STEP = 128 / ES;
     constexpr bool PC = p_columns(OP), QC = q_columns(OP);
@@ -858,8 +858,8 @@ template <int OP, int MI, int F> __global__ __launch_bounds__(64 * FEW_WAVES) vo
 // Products of many rows with sums of at most 1024 bytes are bound by their rows, not by arithmetic, and in tiles a workgroup mostly waits: for its first loads,
 // for its last stores.  Here W stays: a workgroup keeps up to 128 KB of it (blocks of 64 columns) in LDS, and each of its eight wavefronts walks over rows, 16 at a
 // time, on its own: their 16 x S operands come straight into registers, one walk ahead, no barrier in the loop, and 64 columns after the other are
-// multiplied and stored.  Over 3e5 rows, us, tiles and this: 64 by 64 35 and 21, K = 256 by 47 102 and 61; 256 by 256 139 and 150.  It takes rows at any
-// alignment (ODD: that are no whole dwords): 65 by 65 63 and 48; 8192 rows of them 12.9 and 7.6.
+// multiplied and stored.  Over 3e5 rows, GELU and residual (ReLU alone), us, tiles and this: 64 by 64 42 and 26 (29 and 16), K = 256 by 47 93 and 64 (61 and 47); 256 by 256
+// 135 and 140 (84 and 101).  It takes rows at any alignment (ODD: that are no whole dwords): 65 by 65 74 and 52 (56 and 33); 8192 rows of them 15.6 and 7.5.
 //   CHUNKS: of 64 bytes of s; BLOCKS: of 64 columns that LDS has room for at CHUNKS.  fp32 results: fragment f has columns 16 f + t, so that a store has 64
 // bytes of a row; bf16: lane g has 16 columns, 32 bytes of its row.
 constexpr int TALL_WAVES = 8;
@@ -1012,12 +1012,14 @@ constexpr int CUS = 256;
 // Whether a launch of so many workgroups of `threads` holds fewer than 2^32 work-items, which is the limit.
 bool launch_holds(double workgroups, int threads) { return workgroups * threads < 4294967296.0; }
 
-// The tile and the number of splits of the sums with the least time by a model of it: workgroups in rounds of what fits the CUs, 15 TB/s for the tiles' loads,
-// and for splits a second launch that reads the partial sums (1.5 us; two launches cost the host 9.5).  Against the best of all tiles and splits, on 90
-// products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 13 % at most, dw 2.0 % and 26 %.  Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096,
-// K = 4096: 256 x 256 211, 128 x 128 258; 512 x 256, K = 256: 64 x 128 8.0, 256 x 256 15.8; dw over 8192 rows, 256 x 256: 64 x 128 in 16 splits 14.6, unsplit 81.
+// What linear_tall_kernel can take.
 bool may_be_tall(int op, int64_t S) { return (op == FWD_BF16 || op == GRAD_X) && S >= 8 && (S <= 256 || (S <= 512 && S % 2 == 0)); }
 
+// The tile and the number of splits of the sums with the least time by a model of it: workgroups in rounds of what fits the CUs, 15 TB/s for the tiles' loads,
+// and for splits a second launch that reads the partial sums (1.5 us; two launches cost the host 9.5).  Against the best of all tiles and splits, on 90
+// products (forward of 128 .. 3e5 rows and dw): forward 1.3 % slower in the mean and 13 % at most, dw 2.0 % and 26 %.
+//   Examples, us: forward 512 x 4096, K = 4096: 128 x 128 in 2 splits 38, unsplit 47, 256 x 256 (4) 50; 8192 x 4096, K = 4096: 256 x 256 211, 128 x 128 258; 512 x 256,
+// K = 256: 64 x 128 8.0, 256 x 256 15.8; dw over 8192 rows, 256 x 256: 64 x 128 in 16 splits 13.7, unsplit 81.
 //   By way of registers (rows that are no whole units): 128 x 128 tiles, whose step then takes 2.1 us alone and 3.1 with another on the CU, and 9 us at least.
 double search_tiles(LinearPlan& p, int op, int64_t I, int32_t J, bool registers) {
     double best = 0.0;
@@ -1083,8 +1085,8 @@ LinearPlan plan_of(int op, int64_t I, int32_t J, int64_t S) {
         double packed = search_tiles(whole, op, I, J, false), tiles = search_tiles(p, op, I, J, true);
         if (may_be_tall(op, S)) {
             // A wavefront's 16 rows and 64 columns take 0.3 us of a CU up to S = 128, 0.42 up to 256, then 0.35 + 0.0011 S; tiles are held to 4 TB/s for A and for C and
-            // one tensor like it.  us, this and copied tiles: 512 rows, 65 -> 1025 7.5 and 12; 3e5, 65 -> 65 48 and 57, 500 -> 129 189 and 293; 44 713, 376 -> 8175
-            // 1359 and 821.
+            // one tensor like it.  us, this and the better tiles: 512 rows, 65 -> 1025 7.1 and 15.4; 3e5, 65 -> 65 52 and 74, 500 -> 129 192 and 291; 44 713, 376 -> 8175
+            // 983 and 670.
             const double memory = ((double)I * S * 2.0 + (double)I * J * 4.0) / 4e6;
             const double tall = 6.5 + std::max(1.0, (double)cdiv(I, 16) * (double)cdiv(J, 64) / CUS) * (S <= 128 ? 0.3 : S <= 256 ? 0.42 : 0.35 + 0.0011 * S);
             packed = std::max(packed, memory);

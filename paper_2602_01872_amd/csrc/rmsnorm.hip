@@ -8,7 +8,8 @@
 // read once and every output written once, 16 bytes a lane, a row held in registers by the 8 .. 64 lanes of a wavefront or by a whole workgroup.
 //   Measured: 3e5 x 256 fp32 with the residual to bf16 183 us (5.9 TB/s), 8192 x 8192 bf16 with the residual to 8 bits 93 us (5.1 TB/s), 1e5 x 1004 bf16 to 8 bits
 // without a norm 53 us (5.7 TB/s), the gradient over 3e5 x 256 with the residual's 200 us (5.4 TB/s, 5 us of it the sum over 1024 workgroups' rows for the weight).
-// Rows of 257 instead of 256 bf16 146 and 105 us, of 8191 instead of 8192 119 and 104, of fp32 the same.
+// Odd widths: 3e5 rows of 257 instead of 256 bf16 150 and 104 us, fp32 223 and 209, the gradient bf16 132 and 119, fp32 281 and 199 (its lanes are half empty);
+// 8192 rows of 8191 instead of 8192 bf16 to 8 bits 116 and 93, bf16 125 and 93, fp32 the same, the gradient bf16 153 and 118, fp32 187 and 185.
 #include "common.h"
 
 namespace grp {
@@ -76,7 +77,7 @@ template <int V, typename T> __device__ __forceinline__ void store_v(T* p, const
     }
 }
 
-// Sums (or unsigned maxima) over the G lanes of a row; G = 64 * waves: by way of LDS (`turn`: which of the kernel's reductions this is).
+// Sums (or unsigned maxima) over the G lanes of a row; G = 64 * waves: by way of LDS, which is read until the workgroup's next barrier: an array for each call.
 template <int G, typename T, class Op> __device__ __forceinline__ T row_reduce(T v, Op op, T* lds /*[G / 64]*/) {
 #pragma unroll
     for (int o = 1; o < (G < 64 ? G : 64); o <<= 1) v = op(v, __shfl_xor(v, o, 64));
@@ -246,6 +247,13 @@ __global__ __launch_bounds__(norm_threads(G)) void rmsnorm_kernel(NormArgs a) {
 // keeps five values of every column: half a wavefront and four), then workgroups.  f(G, P) gets them as constants; false: too wide.  us, this and another:
 //   3e5 x 256 bf16 norm 105, a quarter of the lanes with four units 117; 3e5 x 500 200 and 242; 1e5 x 1004 norm, 64 lanes with two 148, 32 with four 159, 256 with
 //   one 164; its gradient, 32 with four 157, 64 with two 183; 2e4 x 4096 norm, 256 with two 116, 1024 with one 138; 8192 x 8192, 1024 with one 93, 256 with four 104.
+// On both sides of each border, bf16, 2^26 elements, norm and gradient:
+//   128 units, 64 with two (32 with four) 95 and 104, 256 with one 107 and 115; 129, 256 with one 116 and 121, 64 with four 103 and 124; 192 91 and 102, 100 and 106
+//   256 units, 256 with one 89 and 105, with two 90 and 106;  257, with two 106 and 117, with four 124 and 173
+//   513 units, 256 with four 107 and 132, 1024 with one 121 and 134;  768, 101 and 114, 95 and 121;  769, 1024 with one 97 and 125, 256 with four 109 and 124
+//   1024 units, 1024 with one 92 and 117, with two 94 and 150
+// fp32 rows are within 4 % of the better one, but for the gradient of 65 .. 128 units: 32 with four 122 .. 100, 64 with two 93 .. 90.  Above 2048 units the gradient's registers
+// no longer hold a row: 8192 x 16384 bf16 251 us (4.3 TB/s), 8192 x 32768 1530 us (1.4 TB/s).
 template <int I> using int_c = std::integral_constant<int, I>;
 template <bool GRAD, class F> bool for_row_shape(int64_t units, F f) {
     if (units <= 8) f(int_c<8>(), int_c<1>());
@@ -439,7 +447,7 @@ GradPlan grad_plan(int64_t rows, int32_t width, bool wide /*both types bf16*/) {
     p.units = (int)cdiv(width, p.V);
     int rows_wg = 1;
     for_row_shape<true>(p.units, [&](auto G, auto) { rows_wg = norm_threads(G) / G; });
-    // 1024 workgroups: four a CU, as many as run at once
+    // 1024 workgroups: of 256 threads four a CU, as many as run at once; of 1024 threads (rows of more than 768 units) one or two a CU run at a time
     p.wgs = (int)std::min<int64_t>(1024, cdiv(rows, rows_wg));
     return p;
 }
