@@ -622,7 +622,7 @@ grp_status grp_linear_dw(int64_t M, int32_t N, int32_t K, const void* A, int64_t
  * memory, made once for a model's gradient buffers (synchronous); calls that use one handle must not overlap in time.
  *   src, dst HOST arrays of DEV pointers (dst NULL: in place; an entry equal to src's: that one in place), counts HOST elements,
  *   dtypes HOST GRP_DTYPE_FP32 / _BF16.  The arrays themselves are copied; the tensors are the caller's and have to outlive the handle.
- *   Tensors must not overlap each other.  Errors: GRP_EINVAL, GRP_EUNSUPPORTED (more than 2^38 elements), GRP_ENOMEM, GRP_EHIP. */
+ *   Tensors must not overlap each other.  A captured call reads the handle at every replay: it is destroyed after the last.  Errors: GRP_EINVAL, GRP_EUNSUPPORTED (more than 2^38 elements), GRP_ENOMEM, GRP_EHIP. */
 typedef struct grp_gradients_s grp_gradients_t;
 grp_status grp_gradients_create(int32_t tensors, const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes,
                                 grp_gradients_t** out);

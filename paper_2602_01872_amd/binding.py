@@ -599,7 +599,7 @@ def grp_linear_dw(M, N, K, A, lda, dZ, lddz, dW, lddw, db, workspace, stream=Non
 
 
 class Gradients:
-    """Owns a grp_gradients_t handle (the tensors of a model's gradient) and keeps the tensors alive."""
+    """Owns a grp_gradients_t handle (the tensors of a model's gradient) and keeps the tensors alive.  It has to outlive the graphs that captured a call with it."""
 
     def __init__(self, handle: int, tensors):
         self.handle, self._keep = handle, tensors
