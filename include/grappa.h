@@ -559,7 +559,8 @@ grp_status grp_gemm_tn(int64_t M, int32_t K, int32_t N, const void* A, int64_t l
  * aligned rows are faster.  Every call is asynchronous on its stream, allocates nothing and may be captured in a HIP graph (but
  * grp_gradients_create / _destroy).  All arithmetic is fp32 at least, but for the sums of e4m3 products whose C is bf16 (grp_linear);
  * each output is rounded once.  No atomics: equal inputs, equal bits.  Infinities and NaN come out as the formulas have them in fp32:
- * the squares of a row of numbers beyond 1.8e19 are infinite there, and its norm makes zeros. */
+ * the squares of a row of numbers beyond 1.8e19 are infinite there, and its norm makes zeros; those of numbers below 1e-23 are zero,
+ * and without an eps its norm makes infinities. */
 
 /* h = x + r;  y = h / sqrt(mean(h^2) + eps) * weight, row by row (y from h before it is rounded).
  *   x, r, h  DEV [rows x width] of x_dtype (fp32 or bf16); r NULL: h = x; h NULL: not written; h may be x or r (equal pitches)

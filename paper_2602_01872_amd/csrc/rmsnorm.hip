@@ -209,12 +209,16 @@ __global__ __launch_bounds__(norm_threads(G)) void rmsnorm_kernel(NormArgs a) {
         // The bits of |y| order as the numbers do, with infinity above them and NaN above that: a row with a NaN has the scale NaN.
         uint32_t most = 0;
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p) {
+            const UnitAt<V> u(p * G + l, a.width);
+            uint32_t m = 0;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const uint32_t b = __float_as_uint(h[p][e]) & 0x7FFFFFFFu;
-                most = most > b ? most : b;
+                m = m > b ? m : b;
             }
+            if (u.skip < V) most = most > m ? most : m;          // (a lane without a unit has 0 rho, which is NaN where rho is infinite)
+        }
         most = row_reduce<G>(most, [](uint32_t p, uint32_t q) { return p > q ? p : q; }, lds_max);
         float s = __uint_as_float(most) / E4M3_MAX;
         s = s < TINY_SCALE ? TINY_SCALE : s;

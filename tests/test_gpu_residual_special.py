@@ -154,3 +154,20 @@ def test_tail_of_gelu(g):
         part = (z.abs() >= lo) & (z.abs() <= hi)
         print(f"|z| {lo} .. {hi}: {float(rel[part].max()):.1e}")
     assert bool((rel <= 1.2e-6 + 7.5e-8 * z.double().square()).all())
+
+
+@pytest.mark.parametrize("width", [3, 8, 40, 100, 256, 300, 1003, 3000, 5000])
+@pytest.mark.parametrize("t", [torch.float32, BF16])
+def test_scales_of_rows_whose_squares_vanish(g, width, t):
+    """Without an eps the formula in fp32 divides by zero: y is infinite, or NaN where h is zero, and the 8-bit row's scale is y's, whatever lanes hold no column."""
+    x = torch.full((3, width), 1e-30, device=DEV)
+    x[1] = 0
+    x[2] = 1
+    x = x.to(t)
+    code = g.DTYPE_FP32 if t is torch.float32 else g.DTYPE_BF16
+    y, q, scale = torch.empty(3, width, device=DEV), torch.empty(3, width, device=DEV, dtype=torch.float8_e4m3fn), torch.empty(3, device=DEV)
+    g.grp_rmsnorm(3, width, x, width, code, None, 0, None, 0.0, None, 0, y, width, g.DTYPE_FP32)
+    g.grp_rmsnorm(3, width, x, width, code, None, 0, None, 0.0, None, 0, q, width, g.DTYPE_E4M3, scale)
+    assert bool(y[0].isinf().all()) and bool(y[1].isnan().all())
+    assert float(scale[0]) == INF and bool(scale[1].isnan()) and abs(float(scale[2]) * 448 - 1) < 1e-6
+    assert bool(q[:2].float().isnan().all()) and bool((q[2].float() == 448).all())
