@@ -127,3 +127,17 @@ def test_a_captured_pass_keeps_its_workspace(g):
         step(big, big)
         junk = torch.full((64 << 20,), 255, dtype=torch.uint8, device=DEV)     # takes what was given back
         del junk
+
+
+def test_no_rows(g):
+    b = g.ResidualBlocks(64, 128, 2, 50, seed=1)
+    x = rows_of(50, 64)
+    b.forward(x)
+    b.backward(x)
+    none = x[:0]
+    assert b.forward(none).shape == (0, 64) and b.serve(none).shape == (0, 64)
+    b.grad.fill_(7)
+    assert b.backward(none).shape == (0, 64)
+    assert bool((b.grad == 0).all())
+    with pytest.raises(ValueError):
+        b.backward(x)
