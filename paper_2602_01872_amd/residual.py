@@ -68,18 +68,19 @@ class ResidualBlocks:
     def refresh(self):
         """Makes the weights' copies anew: to be called after ``theta`` was written by what torch does not see."""
         self._round_weights()
+        self._quantized = None
         if self._served is not None:
             self._weights8()
 
     def _seen(self):
-        """The writes of ``theta`` that copies made now have seen: none where a graph is captured, which makes them at its replays."""
+        """The count of writes of ``theta`` that copies made now have seen: none where a graph is captured, which makes them at its replays."""
         return None if self.theta.is_cuda and torch.cuda.is_current_stream_capturing() else self.theta._version
 
     def _round_weights(self):
         for i, p in enumerate(self.params):
             self.w1[i].copy_(p[1])
             self.w2[i].copy_(p[3])
-        self._rounded, self._quantized = self._seen(), None
+        self._rounded = self._seen()
 
     def _room(self, nbytes: int):
         """A workspace for the calls that follow on the current stream (kept by a graph that is captured as long as it lives)."""
@@ -133,6 +134,7 @@ class ResidualBlocks:
         self.steps += 1
         g.grp_optimizer_step(opt, self.theta.numel(), self.steps, self.theta, self.grad, self.m, self.v)
         self._round_weights()
+        self._quantized = None              # (made anew by the next serve)
         return self.norm
 
     def _weights8(self):

@@ -164,6 +164,13 @@ def test_weights_are_rounded_only_when_they_changed(ops, monkeypatch):
     b.theta.mul_(2)
     results(b, x)
     assert calls.count(FP32) == 4
+    b.theta.mul_(2)
+    b.serve(x)
+    results(b, x)                            # forward rounds its own copies; those in 8 bits, which serves on other streams may be reading, stay
+    assert calls.count(FP32) == 8
+    b.step(None, 1.0)
+    results(b, x)
+    assert calls.count(FP32) == 12
 
 
 def test_the_weights_copies_stay_where_they_are(ops, monkeypatch):
