@@ -7,7 +7,7 @@ Activations and the weights' copies are bf16, master weights, gradients and the 
 8 bits, with weights quantized once, by the 8-bit matrix instructions, whose sums are shorter than fp32 (``grp_linear`` in ``grappa.h``).
 
 Parameters are set by writing into ``theta`` or its views ``params``: the next ``forward`` or ``serve`` makes the weights' copies anew.  That goes by torch's own
-count of writes, which a kernel of the user's own, a collective, a replayed graph and ``.data`` pass by: ``refresh()`` has to follow these.  A captured pass
+count of writes, which a kernel (``grp_optimizer_step`` on ``theta``), a collective, a replayed graph and ``.data`` pass by: ``refresh()`` has to follow these.  A captured pass
 reads the copies at their places, as they are when it is replayed: after a write, ``refresh()`` comes before the replay.
 
 Streams: ``forward``, ``backward`` and ``step`` work on what the object keeps, so they are ordered one after another by the caller, as calls on one stream are.
@@ -84,7 +84,7 @@ class ResidualBlocks:
 
     def _room(self, nbytes: int):
         """A workspace for the calls that follow on the current stream (kept by a graph that is captured as long as it lives)."""
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.theta.device)
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.theta.device) if nbytes else None
 
     def _linear(self, m, n, k, a, w, bias, act, r, c, z):
         ws = self._room(g.grp_linear_workspace_bytes(g.LINEAR_FORWARD, m, n, k, g.DTYPE_BF16))
@@ -117,10 +117,10 @@ class ResidualBlocks:
         if m != self._kept:
             raise ValueError(f"the gradient has {m} rows, the last forward pass {'was not made' if self._kept is None else f'had {self._kept}'}")
         self.dh[:m].copy_(dout)
+        bytes_ = [g.grp_linear_workspace_bytes(kind, m, *nk, g.DTYPE_BF16) for kind in (g.LINEAR_DX, g.LINEAR_DW) for nk in ((d, f), (f, d))]
+        ws = self._room(max(bytes_ + [g.grp_rmsnorm_backward_workspace_bytes(m, d)]))
         for i in reversed(range(self.depth)):
             p, q = self.params[i], self.grads[i]
-            bytes_ = [g.grp_linear_workspace_bytes(kind, m, *nk, g.DTYPE_BF16) for kind in (g.LINEAR_DX, g.LINEAR_DW) for nk in ((d, f), (f, d))]
-            ws = self._room(max(bytes_ + [g.grp_rmsnorm_backward_workspace_bytes(m, d)]))
             g.grp_linear_dx(m, d, f, self.dh, d, self.w2[i], d, self.act, self.z[i], f, self.dz, f, g.DTYPE_BF16, ws)
             g.grp_linear_dw(m, d, f, self.a[i], f, self.dh, d, q[3], d, q[4], ws)
             g.grp_linear_dx(m, f, d, self.dz, f, self.w1[i], f, g.ACT_NONE, None, 0, self.dy, d, g.DTYPE_BF16, ws)
